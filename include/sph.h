@@ -99,7 +99,8 @@ const char* sph_status_string(sph_status status);
 
 /* Pre-size the context's scratch for calls up to these sizes so that later
  * calls allocate nothing (required before capturing calls into a CUDA
- * graph).  max_d is the largest of d_h and d_l. */
+ * graph).  max_d is the largest of d_h and d_l (and of the d of the operators
+ * on a vocabulary table; their tokens count as rows). */
 sph_status sph_reserve(sph_ctx* ctx, int64_t max_rows, int64_t max_n_keep,
                        int64_t max_d);
 
@@ -246,6 +247,7 @@ enum {
   SPH_PROF_SAMPLE = 3,      /* softmax / inverse-CDF draw                    */
   SPH_PROF_VERIFY = 4,      /* speculative acceptance                        */
   SPH_PROF_PREP = 5,        /* operand preparation (hidden-state splits)     */
+  SPH_PROF_TABLE = 6,       /* operators on a vocabulary table               */
   SPH_PROF_CLASSES = 8
 };
 
@@ -533,6 +535,118 @@ sph_status sph_verify_draft(sph_ctx* ctx,
                             const float* draft_probs,
                             uint64_t seed, uint64_t offset,
                             int32_t* n_accepted, int32_t* next_token);
+
+/* ---- operators on a vocabulary table ------------------------------------
+ *
+ * The table W [V, d] that a split head multiplies with (W_h, W_l or the whole
+ * of Eq. 9) is also what the next step's inputs are read from (Eq. 1, the
+ * token term) and what local adaptation trains (Eq. 20's base weights).  These
+ * calls hold it in 4 bits, multiply with it, look tokens up in it, and make its
+ * gradient.  They follow the conventions above; the sizes they refuse are
+ * d above 2^20, rows or tokens above 2^20 (quantisation: rows up to 2^31 - 1). */
+
+/* Element type of a table's or a result's rows. */
+typedef enum sph_tab_type {
+  SPH_TAB_BF16 = 0,
+  SPH_TAB_FP32 = 1,
+  SPH_TAB_FP16 = 2,
+  SPH_MX4_E8M0 = 3,         /* e2m1 codes, one e8m0 scale per 32 columns     */
+  SPH_MX4_E4M3 = 4          /* e2m1 codes, one e4m3 scale per 16 columns and a
+                               power of two per row                          */
+} sph_tab_type;
+
+/* Rows held in microscaled 4-bit floating point (device pointers, the
+ * caller's).  Column c of row r stands for
+ *   e2m1(nibble c & 1 of codes[r * ld_codes + c / 2]) * scale of block
+ *   c / block in scales[r * ld_scales + c / block] * row_scale[r]
+ * (nibble 0 the low half; block 32 or 16; no row_scale for SPH_MX4_E8M0).
+ * codes and scales start on 16 bytes, ld_codes and ld_scales (bytes) are
+ * multiples of 16, ld_codes >= 16 * ceil(d / 32), ld_scales >= 16 *
+ * ceil(ceil(d / block) / 16).  The codes of columns d .. 32 * ceil(d / 32) - 1 are
+ * zeros; what follows the last scale of a row is not used. */
+typedef struct sph_mx4 {
+  void* codes;
+  int64_t ld_codes;
+  void* scales;
+  int64_t ld_scales;
+  float* row_scale;
+  int64_t rows;
+  int64_t d;
+  int32_t format;           /* SPH_MX4_E8M0 or SPH_MX4_E4M3                  */
+} sph_mx4;
+
+/* Quantise x [out->rows, out->d] (bf16, fp32 or fp16, row stride ld_x
+ * elements) into *out:
+ *   SPH_MX4_E8M0  scale = 2^max(floor(log2(amax)) - 2, -126)
+ *   SPH_MX4_E4M3  row_scale = 2^k, the least with amax(row) <= 2688 * 2^k (k in
+ *                 [-110, 116]; 1 for a row of zeros), scale = amax / 6 / 2^k
+ *                 rounded to e4m3
+ *   code = the e2m1 value (0, 0.5, 1, 1.5, 2, 3, 4, 6) nearest to |x| / (scale *
+ *                 row_scale), ties to the even code, saturating at 6
+ * with amax a block's largest magnitude.  A block that holds a NaN or an
+ * infinity gets a NaN scale and stands for NaN throughout; amax(row) is that of
+ * the other blocks.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sph_status sph_mx4_quantize(sph_ctx* ctx, const void* x, sph_tab_type x_type,
+                            int64_t ld_x, const sph_mx4* out);
+
+/* Logits over the kept rows of a table held in 4 bits:
+ *   out[r, j] = sum_c X[r, c] * W[keep_ids[j], c] (+ bias[keep_ids[j]])
+ * where X is h held in W's own format as a sum of `planes` terms (1 to 4): the
+ * first quantises h as sph_mx4_quantize does, each further one quantises what
+ * the terms before it left over, in units of the first one's row_scale.  One
+ * term is the 4-bit product; with each further one the hidden states' rounding
+ * shrinks some tenfold.  Products add in fp32.
+ *   h      [rows, W->d] bf16, fp32 or fp16, row stride ld_h elements (a slice
+ *          of wider rows, any start).
+ *   bias   fp32 [W->rows] or NULL.  keep_ids, n_keep as for
+ *          sph_partial_logits, with V = W->rows.
+ *   out    fp32 or bf16 [rows, n_keep], row stride ld_out elements; fp32 logits
+ *          are what sph_verify_draft takes.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA, OOM. */
+sph_status sph_mx4_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type,
+                          int64_t rows, int64_t ld_h, const sph_mx4* W,
+                          const float* bias, const int32_t* keep_ids,
+                          int64_t n_keep, int planes, void* out,
+                          sph_tab_type out_type, int64_t ld_out);
+
+/* Rows of a table by token (Eq. 1, the token term, scaled):
+ *   out[t, :] = scale * table[tokens[t], :]
+ * rounded once to out_type (bf16, fp32, fp16).  A token equal to padding_id
+ * gives a row of zeros (so does one outside [0, V), which sph_sync reports as
+ * SPH_ERR_INVALID_ARG); -1 for no padding within the vocabulary.
+ *   tokens int32 [n_tokens], n_tokens >= 0;  table bf16, fp32 or fp16 [V, d],
+ *   row stride ld_table elements;  out [n_tokens, d], row stride ld_out.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sph_status sph_embed(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
+                     const void* table, sph_tab_type table_type, int64_t V,
+                     int64_t d, int64_t ld_table, float scale,
+                     int64_t padding_id, void* out, sph_tab_type out_type,
+                     int64_t ld_out);
+
+/* The same from a table held in 4 bits.  tokens NULL takes its first n_tokens
+ * rows in order (with scale 1: the values that the table stands for, exact in
+ * bf16 and fp32 unless they leave the type's range). */
+sph_status sph_embed_mx4(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
+                         const sph_mx4* table, float scale,
+                         int64_t padding_id, void* out, sph_tab_type out_type,
+                         int64_t ld_out);
+
+/* Gradient of a table from the gradients of the looked-up rows:
+ *   d_table[v, :] = scale * sum over {t : tokens[t] = v} of d_out[t, :]
+ * for every row v (zeros where no token is v); with accumulate != 0 the sums are
+ * added to what d_table holds, and rows without a token are not touched.  Sums
+ * are fp32, rounded once to table_type, and added in an order that the tokens
+ * alone decide: equal inputs give equal bits.  Tokens equal to padding_id take
+ * no part (nor do ones outside [0, V), which sph_sync reports).
+ *   d_out [n_tokens, d] bf16, fp32 or fp16, row stride ld_d_out;  d_table
+ *   [V, d] bf16, fp32 or fp16, row stride ld_table.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA, OOM. */
+sph_status sph_embed_grad(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
+                          const void* d_out, sph_tab_type d_out_type,
+                          int64_t ld_d_out, int64_t V, int64_t d, float scale,
+                          int64_t padding_id, int accumulate, void* d_table,
+                          sph_tab_type table_type, int64_t ld_table);
 
 #ifdef __cplusplus
 }  /* extern "C" */

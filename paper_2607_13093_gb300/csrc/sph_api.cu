@@ -758,6 +758,11 @@ sph_status sph_reserve(sph_ctx* ctx, int64_t max_rows, int64_t max_n_keep,
   if (f > need) need = f;
   const size_t v = verify_reserve_bytes(max_rows, max_n_keep);
   if (v > need) need = v;
+  // the operators on a vocabulary table
+  const size_t m = sph::mx4_gemm_reserve_bytes(max_rows, max_d);
+  if (m > need) need = m;
+  const size_t t = sph::grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
+  if (t > need) need = t;
   for (int act = 0; act < 2; ++act) {      // a one-chunk split step
     const size_t a = split_scratch_bytes(ctx, max_rows, max_n_keep, max_n_keep, max_d, max_d,
                                          act, sph::W_BF16);
@@ -1277,6 +1282,216 @@ sph_status sph_split_step(sph_ctx* ctx, const float* h, int64_t rows, int64_t ld
   if (e == cudaSuccess) e = cudaStreamWaitEvent(ctx->stream, ev[nchunk + 1], 0);
   if (e != cudaSuccess) return cuda_fail(ctx, e, "joining the endpoint stream");
   return SPH_OK;
+}
+
+// ---- operators on a vocabulary table ----------------------------------------
+namespace {
+
+constexpr int64_t kTabMaxD = 1 << 20, kTabMaxRows = 1 << 20;
+
+int tab_size(int t) { return t == SPH_TAB_FP32 ? 4 : 2; }
+bool tab_dense(int t) { return t == SPH_TAB_BF16 || t == SPH_TAB_FP32 || t == SPH_TAB_FP16; }
+
+// A dense operand of the table operators: type, stride and alignment.
+sph_status check_rows(sph_ctx* ctx, const char* name, const void* p, int type, int64_t d,
+                      int64_t ld) {
+  if (!p) return fail(ctx, SPH_ERR_INVALID_ARG, "%s must be non-NULL", name);
+  if (!tab_dense(type)) return fail(ctx, SPH_ERR_INVALID_ARG, "%s: type %d is not bf16, fp32 or fp16", name, type);
+  if (ld < d) return fail(ctx, SPH_ERR_INVALID_ARG, "%s: row stride %lld below %lld columns", name, (long long)ld, (long long)d);
+  if ((uintptr_t)p % tab_size(type)) return fail(ctx, SPH_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+  return SPH_OK;
+}
+sph_status check_d(sph_ctx* ctx, int64_t d) {
+  if (d < 1) return fail(ctx, SPH_ERR_INVALID_ARG, "d must be >= 1");
+  if (d > kTabMaxD) return fail(ctx, SPH_ERR_UNSUPPORTED, "d=%lld above %lld", (long long)d, (long long)kTabMaxD);
+  return SPH_OK;
+}
+sph_status check_mx4(sph_ctx* ctx, const sph_mx4* w) {
+  if (!w) return fail(ctx, SPH_ERR_INVALID_ARG, "the 4-bit rows must be non-NULL");
+  if (w->format != SPH_MX4_E8M0 && w->format != SPH_MX4_E4M3)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "unknown 4-bit format %d", (int)w->format);
+  sph_status st = check_d(ctx, w->d);
+  if (st) return st;
+  if (w->rows < 1 || w->rows > INT32_MAX)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "rows=%lld of the 4-bit form out of range", (long long)w->rows);
+  if (!w->codes || !w->scales) return fail(ctx, SPH_ERR_INVALID_ARG, "codes and scales must be non-NULL");
+  if ((w->format == SPH_MX4_E4M3) != (w->row_scale != nullptr))
+    return fail(ctx, SPH_ERR_INVALID_ARG, "row_scale goes with SPH_MX4_E4M3, and only with it");
+  const int64_t block = w->format == SPH_MX4_E4M3 ? 16 : 32;
+  const int64_t need_c = (w->d + 31) / 32 * 16, need_s = ((w->d + block - 1) / block + 15) / 16 * 16;
+  if (((uintptr_t)w->codes & 15) || ((uintptr_t)w->scales & 15) || (w->ld_codes & 15) ||
+      (w->ld_scales & 15))
+    return fail(ctx, SPH_ERR_INVALID_ARG, "codes, scales and their row strides must be 16-byte aligned");
+  if (w->ld_codes < need_c || w->ld_scales < need_s)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "rows of %lld columns need %lld bytes of codes and %lld of scales",
+                (long long)w->d, (long long)need_c, (long long)need_s);
+  if (w->ld_codes >= ((int64_t)1 << 40))
+    return fail(ctx, SPH_ERR_UNSUPPORTED, "row stride of the codes too large");
+  return SPH_OK;
+}
+int mx4_format(const sph_mx4* w) { return w->format == SPH_MX4_E4M3 ? 1 : 0; }
+
+sph_status check_lookup(sph_ctx* ctx, int64_t n_tokens, int64_t d, float scale, const void* out,
+                        int out_type, int64_t ld_out) {
+  if (!std::isfinite(scale)) return fail(ctx, SPH_ERR_INVALID_ARG, "scale must be finite");
+  if (n_tokens * ((d + 1023) / 1024) > INT32_MAX)
+    return fail(ctx, SPH_ERR_UNSUPPORTED, "%lld rows of %lld columns in one call", (long long)n_tokens, (long long)d);
+  return check_rows(ctx, "out", out, out_type, d, ld_out);
+}
+sph_status check_tokens(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens) {
+  if (n_tokens < 0 || n_tokens > kTabMaxRows)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "n_tokens=%lld out of [0, 2^20]", (long long)n_tokens);
+  if (!tokens && n_tokens > 0) return fail(ctx, SPH_ERR_INVALID_ARG, "tokens must be non-NULL");
+  return SPH_OK;
+}
+
+}  // namespace
+
+sph_status sph_mx4_quantize(sph_ctx* ctx, const void* x, sph_tab_type x_type, int64_t ld_x,
+                            const sph_mx4* out) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_mx4(ctx, out);
+  if (st) return st;
+  st = check_rows(ctx, "x", x, x_type, out->d, ld_x);
+  if (st) return st;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  const int64_t span = out->format == SPH_MX4_E4M3 ? 256 : 512;    // columns of 16 scale bytes
+  sph::Mx4Quant q{};
+  q.x = x; q.ld_x = ld_x; q.rows = (int)out->rows; q.d = (int)out->d;
+  q.codes = static_cast<uint8_t*>(out->codes); q.ld_codes = out->ld_codes;
+  q.scales = static_cast<uint8_t*>(out->scales); q.ld_scales = out->ld_scales;
+  q.row_scale = out->row_scale;
+  q.scale_cols = (int)((out->d + span - 1) / span * span);
+  q.planes = 1;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_mx4_quant(q, mx4_format(out), x_type, false, ctx->stream);
+                       }), "4-bit quantise launch");
+}
+
+sph_status sph_mx4_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type, int64_t rows,
+                          int64_t ld_h, const sph_mx4* W, const float* bias,
+                          const int32_t* keep_ids, int64_t n_keep, int planes, void* out,
+                          sph_tab_type out_type, int64_t ld_out) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_mx4(ctx, W);
+  if (st) return st;
+  st = check_rows(ctx, "h", h, h_type, W->d, ld_h);
+  if (st) return st;
+  if (rows < 1 || rows > kTabMaxRows)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "rows=%lld out of [1, 2^20]", (long long)rows);
+  st = check_ids(ctx, keep_ids, n_keep, W->rows);
+  if (st) return st;
+  if (planes < 1 || planes > 4) return fail(ctx, SPH_ERR_INVALID_ARG, "planes=%d out of [1, 4]", planes);
+  if (out_type == SPH_TAB_FP16) return fail(ctx, SPH_ERR_UNSUPPORTED, "logits are fp32 or bf16");
+  st = check_rows(ctx, "out", out, out_type, n_keep, ld_out);
+  if (st) return st;
+  if (n_keep > sph::sample_max_n()) return fail(ctx, SPH_ERR_UNSUPPORTED, "n_keep above %d", sph::sample_max_n());
+  if (rows * n_keep > ((int64_t)1 << 40)) return fail(ctx, SPH_ERR_UNSUPPORTED, "rows*n_keep too large");
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  st = host_check_ids(ctx, keep_ids, n_keep, W->rows);
+  if (st) return st;
+  const int fmt = mx4_format(W);
+  st = ensure_scratch(ctx, sph::mx4_gemm_scratch_bytes(rows, n_keep, (int)W->d, planes, fmt));
+  if (st) return st;
+  sph::Mx4Gemm m{};
+  m.x = h; m.ld_x = ld_h; m.rows = (int)rows; m.d = (int)W->d; m.x_type = h_type;
+  m.planes = planes; m.fmt = fmt;
+  m.w_codes = static_cast<const uint8_t*>(W->codes); m.ld_codes = W->ld_codes;
+  m.w_scales = static_cast<const uint8_t*>(W->scales); m.ld_scales = W->ld_scales;
+  m.w_row = W->row_scale; m.V = W->rows; m.bias = bias; m.ids = keep_ids; m.n = (int)n_keep;
+  m.out = out; m.ld_out = ld_out; m.out_type = out_type; m.status = ctx->status;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_mx4_gemm(m, ctx->scratch, ctx->spin_limit,
+                                                     ctx->sm_count, ctx->stream);
+                       }), "4-bit product launch");
+}
+
+sph_status sph_embed(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens, const void* table,
+                     sph_tab_type table_type, int64_t V, int64_t d, int64_t ld_table, float scale,
+                     int64_t padding_id, void* out, sph_tab_type out_type, int64_t ld_out) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_d(ctx, d);
+  if (st) return st;
+  if (V < 1 || V > INT32_MAX) return fail(ctx, SPH_ERR_INVALID_ARG, "V=%lld out of range", (long long)V);
+  st = check_tokens(ctx, tokens, n_tokens);
+  if (st) return st;
+  st = check_rows(ctx, "table", table, table_type, d, ld_table);
+  if (st) return st;
+  if (n_tokens == 0) return SPH_OK;
+  st = check_lookup(ctx, n_tokens, d, scale, out, out_type, ld_out);
+  if (st) return st;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  sph::Lookup a{};
+  a.tokens = tokens; a.n = n_tokens; a.table = table; a.ld_table = ld_table; a.V = V; a.d = (int)d;
+  a.scale = scale; a.padding = padding_id; a.out = out; a.ld_out = ld_out; a.status = ctx->status;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_lookup(a, table_type, out_type, ctx->sm_count, ctx->stream);
+                       }), "lookup launch");
+}
+
+sph_status sph_embed_mx4(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
+                         const sph_mx4* table, float scale, int64_t padding_id, void* out,
+                         sph_tab_type out_type, int64_t ld_out) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_mx4(ctx, table);
+  if (st) return st;
+  if (tokens) {
+    st = check_tokens(ctx, tokens, n_tokens);
+    if (st) return st;
+  } else if (n_tokens < 0 || n_tokens > table->rows) {
+    return fail(ctx, SPH_ERR_INVALID_ARG, "n_tokens=%lld of %lld rows in order", (long long)n_tokens,
+                (long long)table->rows);
+  }
+  if (n_tokens == 0) return SPH_OK;
+  st = check_lookup(ctx, n_tokens, table->d, scale, out, out_type, ld_out);
+  if (st) return st;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  sph::Lookup a{};
+  a.tokens = tokens; a.n = n_tokens;
+  a.table = table->codes; a.ld_table = table->ld_codes;
+  a.scales = static_cast<const uint8_t*>(table->scales); a.ld_scales = table->ld_scales;
+  a.row_scale = table->row_scale; a.V = table->rows; a.d = (int)table->d;
+  a.scale = scale; a.padding = padding_id; a.out = out; a.ld_out = ld_out; a.status = ctx->status;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_lookup(a, table->format, out_type, ctx->sm_count,
+                                                   ctx->stream);
+                       }), "4-bit lookup launch");
+}
+
+sph_status sph_embed_grad(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens, const void* d_out,
+                          sph_tab_type d_out_type, int64_t ld_d_out, int64_t V, int64_t d,
+                          float scale, int64_t padding_id, int accumulate, void* d_table,
+                          sph_tab_type table_type, int64_t ld_table) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_d(ctx, d);
+  if (st) return st;
+  if (V < 1 || V > INT32_MAX) return fail(ctx, SPH_ERR_INVALID_ARG, "V=%lld out of range", (long long)V);
+  st = check_tokens(ctx, tokens, n_tokens);
+  if (st) return st;
+  if (!std::isfinite(scale)) return fail(ctx, SPH_ERR_INVALID_ARG, "scale must be finite");
+  if (n_tokens > 0) {
+    st = check_rows(ctx, "d_out", d_out, d_out_type, d, ld_d_out);
+    if (st) return st;
+  }
+  st = check_rows(ctx, "d_table", d_table, table_type, d, ld_table);
+  if (st) return st;
+  if (n_tokens == 0 && accumulate) return SPH_OK;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  st = ensure_scratch(ctx, sph::grad_scratch_bytes(n_tokens, (int)d, ctx->sm_count));
+  if (st) return st;
+  sph::TableGrad a{};
+  a.tokens = tokens; a.n = (int)n_tokens; a.d_out = d_out; a.ld_d_out = ld_d_out;
+  a.V = (int32_t)V; a.d = (int)d; a.scale = scale; a.padding = padding_id; a.add = accumulate != 0;
+  a.out = d_table; a.ld_out = ld_table; a.status = ctx->status;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_table_grad(a, d_out_type, table_type, ctx->scratch,
+                                                       ctx->sm_count, ctx->stream);
+                       }), "table gradient launch");
 }
 
 }  // extern "C"

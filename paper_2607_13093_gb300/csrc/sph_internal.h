@@ -304,4 +304,97 @@ cudaError_t launch_verify(const float* Z, int sessions, int k, int n,
                           int32_t* next_token, void* scratch, int sm_count,
                           cudaStream_t st, int greedy = 0);
 
+// ---- operators on a vocabulary table ---------------------------------------
+// Element types of their rows (sph_tab_type).
+enum TabType : int { TAB_BF16 = 0, TAB_FP32 = 1, TAB_FP16 = 2, TAB_E8M0 = 3, TAB_E4M3 = 4 };
+
+// Rows to 4 bits (k_mx4.cu).
+struct Mx4Quant {
+  const void* x;            // [rows, d], row stride ld_x elements
+  int64_t ld_x;
+  int rows, d;
+  uint8_t* codes;           // row stride ld_codes bytes; columns d up to a whole 32 are zeros
+  int64_t ld_codes;
+  uint8_t* scales;          // table form: row stride ld_scales bytes
+  int64_t ld_scales;
+  float* row_scale;         // [rows] 2^k, or nullptr
+  int scale_cols;           // columns whose scale bytes are written (zeros past d)
+  int planes;               // terms; 1 in the table form
+  // operand form
+  int64_t plane_codes, plane_scales;    // bytes between terms
+  int tile_rows, groups;    // rows of a tile, 4-byte scale groups of a row
+  int aligned;              // set by the launch: rows start on 16 bytes
+};
+cudaError_t launch_mx4_quant(Mx4Quant a, int fmt, int x_type, bool operand, cudaStream_t st);
+
+// Product with a table held in 4 bits (k_mx4_tc.cu).
+struct Mx4Gemm {
+  const void* x;            // [rows, d], row stride ld_x elements of x_type
+  int64_t ld_x;
+  int rows, d, x_type, planes, fmt;
+  const uint8_t* w_codes;   // [V], row stride ld_codes bytes
+  int64_t ld_codes;
+  const uint8_t* w_scales;  // [V], row stride ld_scales bytes
+  int64_t ld_scales;
+  const float* w_row;       // [V], e4m3 only
+  int64_t V;
+  const float* bias;        // [V] or nullptr
+  const int32_t* ids;       // [n] or nullptr (identity)
+  int n;
+  void* out;                // [rows, n], row stride ld_out elements of out_type
+  int64_t ld_out;
+  int out_type;             // TAB_FP32 or TAB_BF16
+  unsigned* status;
+};
+size_t mx4_gemm_scratch_bytes(int64_t rows, int64_t n, int d, int planes, int fmt);
+size_t mx4_gemm_reserve_bytes(int64_t rows, int64_t d);
+cudaError_t launch_mx4_gemm(const Mx4Gemm& g, void* scratch, long long spin_limit, int sm_count,
+                            cudaStream_t st);
+
+// Lookup of table rows (k_table.cu).
+struct Lookup {
+  const int32_t* tokens;    // [n], or nullptr: rows 0 .. n - 1
+  int64_t n;
+  const void* table;        // [V, d], row stride ld_table elements (4-bit codes: bytes)
+  int64_t ld_table;
+  const uint8_t* scales;    // 4-bit tables: scale bytes, and row scales for e4m3
+  int64_t ld_scales;
+  const float* row_scale;
+  int64_t V;
+  int d;
+  float scale;
+  int64_t padding;          // the id that stands for a row of zeros
+  void* out;                // [n, d], row stride ld_out elements
+  int64_t ld_out;
+  unsigned* status;
+  int spans;                // set by the launch
+};
+cudaError_t launch_lookup(Lookup a, int table_type, int out_type, int sm_count, cudaStream_t st);
+
+// Gradient of a table (k_table.cu).
+struct TableGrad {
+  const int32_t* tokens;    // [n]
+  int n;
+  const void* d_out;        // [n, d], row stride ld_d_out elements
+  int64_t ld_d_out;
+  int32_t V;
+  int d;
+  float scale;
+  int64_t padding;
+  int add;                  // 1: added to what out holds
+  void* out;                // [V, d], row stride ld_out elements
+  int64_t ld_out;
+  unsigned* status;
+  // set by the launch
+  int32_t* keys[2];         // ids and positions; sorted in [0]
+  int32_t* pos[2];
+  float* partial;           // [ranges][2][ld_partial]
+  int64_t ld_partial;
+  int range, groups;        // sorted positions a range, column groups
+};
+size_t grad_scratch_bytes(int64_t n, int d, int sm_count);
+size_t grad_reserve_bytes(int64_t n, int64_t d, int sm_count);
+cudaError_t launch_table_grad(TableGrad a, int src_type, int out_type, void* scratch, int sm_count,
+                              cudaStream_t st);
+
 }  // namespace sph

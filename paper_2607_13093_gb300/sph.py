@@ -16,7 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -40,6 +40,7 @@ SPH_OPT_ENDPOINT_Z = 12
 SPH_OPT_ENDPOINT_ROWS_M = 13
 SPH_OPT_GEMV_QUANTIZE = 14
 SPH_OPT_FEW_ROWS = 15
+SPH_TAB_BF16, SPH_TAB_FP32, SPH_TAB_FP16, SPH_MX4_E8M0, SPH_MX4_E4M3 = 0, 1, 2, 3, 4
 SPH_SAMPLER_CDF, SPH_SAMPLER_GUMBEL = 0, 1
 
 _c_void_p = ctypes.c_void_p
@@ -51,7 +52,7 @@ _sz = ctypes.c_size_t
 
 PROF_CLASSES = 8
 PROF_NAMES = ("cloud_gemm", "quantize", "local_gemm", "sample", "verify",
-              "prep", "reserved6", "reserved7")
+              "prep", "table", "reserved7")
 
 
 class sph_profile(ctypes.Structure):
@@ -67,6 +68,12 @@ PLAN_FIELDS = ("tensor_core", "row_blocks", "block_rows", "tile_ids", "tiles",
 
 class sph_plan(ctypes.Structure):
     _fields_ = [(f, ctypes.c_int32) for f in PLAN_FIELDS]
+
+
+class sph_mx4(ctypes.Structure):
+    _fields_ = [("codes", _c_void_p), ("ld_codes", _i64), ("scales", _c_void_p),
+                ("ld_scales", _i64), ("row_scale", _c_void_p), ("rows", _i64), ("d", _i64),
+                ("format", ctypes.c_int32)]
 
 
 # name -> (restype, argtypes), mirroring include/sph.h
@@ -111,6 +118,15 @@ _SIGNATURES = {
     "sph_verify_draft": (_int, [_c_void_p, _c_void_p, _i64, _i64, _c_void_p,
                                 _i64, _f32, _c_void_p, _c_void_p, _u64, _u64,
                                 _c_void_p, _c_void_p]),
+    "sph_mx4_quantize": (_int, [_c_void_p, _c_void_p, _int, _i64, ctypes.POINTER(sph_mx4)]),
+    "sph_mx4_logits": (_int, [_c_void_p, _c_void_p, _int, _i64, _i64, ctypes.POINTER(sph_mx4),
+                              _c_void_p, _c_void_p, _i64, _int, _c_void_p, _int, _i64]),
+    "sph_embed": (_int, [_c_void_p, _c_void_p, _i64, _c_void_p, _int, _i64, _i64, _i64, _f32,
+                         _i64, _c_void_p, _int, _i64]),
+    "sph_embed_mx4": (_int, [_c_void_p, _c_void_p, _i64, ctypes.POINTER(sph_mx4), _f32, _i64,
+                             _c_void_p, _int, _i64]),
+    "sph_embed_grad": (_int, [_c_void_p, _c_void_p, _i64, _c_void_p, _int, _i64, _i64, _i64, _f32,
+                              _i64, _int, _c_void_p, _int, _i64]),
 }
 
 
@@ -545,6 +561,170 @@ def sph_verify_draft(ctx, target_logits, sessions: int, k: int, draft_tokens,
     return n_accepted, next_token
 
 
+# ---- operators on a vocabulary table ---------------------------------------
+
+_TAB_TYPES = {torch.bfloat16: SPH_TAB_BF16, torch.float32: SPH_TAB_FP32,
+              torch.float16: SPH_TAB_FP16}
+
+
+class Mx4(NamedTuple):
+    """Rows held in microscaled 4-bit floating point (sph_mx4 of the header):
+    codes uint8 [rows, >= 16 ceil(d / 32)], scales uint8 [rows, >= the scales in
+    whole 16 bytes], row_scale fp32 [rows] for SPH_MX4_E4M3 (else None)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    row_scale: Optional[torch.Tensor]
+    d: int
+    format: int
+
+    @property
+    def block(self) -> int:
+        return 16 if self.format == SPH_MX4_E4M3 else 32
+
+
+def mx4_empty(rows: int, d: int, format: int = SPH_MX4_E4M3, device="cuda") -> Mx4:
+    """Room for `rows` rows of d columns in 4 bits."""
+    if format not in (SPH_MX4_E8M0, SPH_MX4_E4M3):
+        raise ValueError("format must be SPH_MX4_E8M0 or SPH_MX4_E4M3")
+    if rows < 1 or d < 1:
+        raise ValueError("rows and d must be >= 1")
+    block = 16 if format == SPH_MX4_E4M3 else 32
+    codes = torch.empty(rows, -(-d // 32) * 16, dtype=torch.uint8, device=device)
+    scales = torch.empty(rows, -(-d // (16 * block)) * 16, dtype=torch.uint8, device=device)
+    row = torch.empty(rows, dtype=torch.float32, device=device) \
+        if format == SPH_MX4_E4M3 else None
+    return Mx4(codes, scales, row, d, format)
+
+
+def _mx4(w: Mx4, dev) -> sph_mx4:
+    """The C form of w, whose buffers hold what its rows and d say."""
+    codes, scales, row, d, fmt = w
+    if codes.device != dev or scales.device != dev or codes.device.type != "cuda":
+        raise ValueError(f"the 4-bit rows are on {codes.device} and {scales.device}, not on {dev}")
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise ValueError("codes and scales must be uint8")
+    rows = codes.shape[0]
+    if scales.shape[0] != rows:
+        raise ValueError(f"{rows} rows of codes, {scales.shape[0]} of scales")
+    block = 16 if fmt == SPH_MX4_E4M3 else 32
+    if codes.shape[1] < -(-d // 32) * 16 or scales.shape[1] < -(-d // (16 * block)) * 16:
+        raise ValueError(f"codes and scales are too narrow for {d} columns")
+    if row is not None:
+        _need(row, torch.float32, "row_scale")
+        _dense(dev, (row, "row_scale", rows))
+    # (a single row's stride says nothing: any width that holds it)
+    return sph_mx4(codes.data_ptr(), _ld(codes) if rows > 1 else -(-codes.shape[1] // 16) * 16,
+                   scales.data_ptr(), _ld(scales) if rows > 1 else -(-scales.shape[1] // 16) * 16,
+                   _ptr(row), rows, d, fmt)
+
+
+def _rows(t, name, dev=None):
+    """(type, row stride) of a dense 2-D operand of the table operators."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if dev is not None and t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, not on {dev}")
+    typ = _TAB_TYPES.get(t.dtype)
+    if typ is None:
+        raise ValueError(f"{name} must be bfloat16, float32 or float16, got {t.dtype}")
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be 2-D with unit inner stride")
+    # (the stride of a single row is any: it is not stepped over)
+    return typ, (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+
+
+def _result(out, shape, dtype, dev, name):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(out.shape)}")
+    return out
+
+
+def sph_mx4_quantize(ctx, x, format=SPH_MX4_E4M3, *, out: Optional[Mx4] = None) -> Mx4:
+    """Rows of x [R, d] (bf16, fp32 or fp16, any row stride) in 4 bits."""
+    typ, ld = _rows(x, "x")
+    if out is None:
+        out = mx4_empty(x.shape[0], x.shape[1], format, x.device)
+    elif out.codes.shape[0] != x.shape[0] or out.d != x.shape[1] or out.format != format:
+        raise ValueError(f"out does not hold {tuple(x.shape)} in format {format}")
+    c = _mx4(out, x.device)
+    _check(ctx, lib.sph_mx4_quantize(ctx, x.data_ptr(), typ, ld, c))
+    return out
+
+
+def sph_mx4_dequantize(ctx, w: Mx4, *, out=None, dtype=torch.bfloat16):
+    """The values that w stands for, [rows, d]."""
+    c = _mx4(w, w.codes.device)
+    out = _result(out, (c.rows, w.d), dtype, w.codes.device, "out")
+    typ, ld = _rows(out, "out", w.codes.device)
+    _check(ctx, lib.sph_embed_mx4(ctx, None, c.rows, c, 1.0, -1, out.data_ptr(), typ, ld))
+    return out
+
+
+def sph_mx4_logits(ctx, h, W: Mx4, *, keep_ids=None, bias=None, planes=2, out=None,
+                   dtype=torch.float32):
+    """Logits [R, n] of hidden states h [R, d] over the kept rows of a table in
+    4 bits; h is held as `planes` terms of W's format.  fp32 or bf16."""
+    dev = h.device
+    typ, ld = _rows(h, "h")
+    c = _mx4(W, dev)
+    if h.shape[1] != W.d:
+        raise ValueError(f"h has {h.shape[1]} columns, the table {W.d}")
+    n = c.rows if keep_ids is None else keep_ids.numel()
+    _need(keep_ids, torch.int32, "keep_ids")
+    _need(bias, torch.float32, "bias")
+    _dense(dev, (keep_ids, "keep_ids", n), (bias, "bias", c.rows))
+    out = _result(out, (h.shape[0], n), dtype, dev, "out")
+    otyp, old = _rows(out, "out", dev)
+    _check(ctx, lib.sph_mx4_logits(ctx, h.data_ptr(), typ, h.shape[0], ld, c, _ptr(bias),
+                                   _ptr(keep_ids), n, int(planes), out.data_ptr(), otyp, old))
+    return out
+
+
+def sph_embed(ctx, tokens, table, *, scale=1.0, padding_id=-1, out=None, dtype=None):
+    """scale * table[tokens] as [T, d]: tokens int32 [T], table a tensor [V, d]
+    (bf16, fp32 or fp16) or an Mx4.  dtype: the table's own, bf16 for an Mx4."""
+    dev = tokens.device
+    _need(tokens, torch.int32, "tokens")
+    _dense(dev, (tokens, "tokens", 0))
+    n = tokens.numel()
+    if isinstance(table, Mx4):
+        c = _mx4(table, dev)
+        out = _result(out, (n, table.d), dtype or torch.bfloat16, dev, "out")
+        typ, ld = _rows(out, "out", dev)
+        _check(ctx, lib.sph_embed_mx4(ctx, tokens.data_ptr() if n else None, n if n else 0, c,
+                                      float(scale), int(padding_id), out.data_ptr(), typ, ld))
+        return out
+    ttyp, tld = _rows(table, "table", dev)
+    V, d = table.shape
+    out = _result(out, (n, d), dtype or table.dtype, dev, "out")
+    typ, ld = _rows(out, "out", dev)
+    _check(ctx, lib.sph_embed(ctx, tokens.data_ptr(), n, table.data_ptr(), ttyp, V, d, tld,
+                              float(scale), int(padding_id), out.data_ptr(), typ, ld))
+    return out
+
+
+def sph_embed_grad(ctx, tokens, d_out, V: int, *, scale=1.0, padding_id=-1, accumulate=False,
+                   out=None, dtype=torch.float32):
+    """The table's gradient [V, d] of sph_embed from d_out [T, d]; accumulate
+    adds it to `out` (rows without a token are not touched)."""
+    dev = d_out.device
+    _need(tokens, torch.int32, "tokens")
+    _dense(dev, (tokens, "tokens", d_out.shape[0]))
+    styp, sld = _rows(d_out, "d_out")
+    if tokens.numel() != d_out.shape[0]:
+        raise ValueError(f"{tokens.numel()} tokens, {d_out.shape[0]} rows of d_out")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    out = _result(out, (int(V), d_out.shape[1]), dtype, dev, "out")
+    typ, ld = _rows(out, "out", dev)
+    _check(ctx, lib.sph_embed_grad(ctx, tokens.data_ptr(), tokens.numel(), d_out.data_ptr(), styp,
+                                   sld, int(V), d_out.shape[1], float(scale), int(padding_id),
+                                   1 if accumulate else 0, out.data_ptr(), typ, ld))
+    return out
+
+
 class Context:
     """A library context on `device`, issuing work on torch's current
     stream of that device (re-read at every call)."""
@@ -584,6 +764,26 @@ class Context:
     def split_step(self, *a, **kw):
         self._follow_stream()
         return sph_split_step(self.handle, *a, **kw)
+
+    def mx4_quantize(self, *a, **kw):
+        self._follow_stream()
+        return sph_mx4_quantize(self.handle, *a, **kw)
+
+    def mx4_dequantize(self, *a, **kw):
+        self._follow_stream()
+        return sph_mx4_dequantize(self.handle, *a, **kw)
+
+    def mx4_logits(self, *a, **kw):
+        self._follow_stream()
+        return sph_mx4_logits(self.handle, *a, **kw)
+
+    def embed(self, *a, **kw):
+        self._follow_stream()
+        return sph_embed(self.handle, *a, **kw)
+
+    def embed_grad(self, *a, **kw):
+        self._follow_stream()
+        return sph_embed_grad(self.handle, *a, **kw)
 
     def sync(self):
         sph_sync(self.handle)
