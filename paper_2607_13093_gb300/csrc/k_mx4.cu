@@ -1,6 +1,6 @@
 // Rows into microscaled 4-bit floating point: the table form (codes and scales
-// row by row) and the operand form of the 4-bit product, whose scales lie as
-// the tensor cores read them and which holds a row as the sum of several
+// row by row) and the operand form of the 4-bit product, whose scales lie
+// stage by stage as it copies them and which holds a row as the sum of several
 // terms, each the 4-bit form of what the terms before it left over.
 //
 // Bound by memory: an element is read once (2 or 4 bytes) and leaves 4.5 or
@@ -96,19 +96,19 @@ quant_kernel(const Mx4Quant a) {
     row_exp = mx4_row_exp(top);
   }
   if (t == 0 && a.row_scale) a.row_scale[row] = exp2_int(row_exp);
-  int64_t at_scale;           // where the row's scale words start, and how far apart they are
-  int step_scale;
+  // the row's scale words: word i at at_scale + i / tile_words * step + i % tile_words
+  // words (table form: one after another)
+  int64_t at_scale, step;
+  int words;
   if constexpr (OPERAND) {
-    // tile of a.tile_rows rows: per 4-byte group of scales a chunk of 512 bytes
-    // for each 128 rows, in it row r at (r % 32) * 16 + (r / 32) * 4
     const int tile = (int)(row / a.tile_rows), r = (int)(row % a.tile_rows);
-    const int chunks = (a.tile_rows + 127) / 128;
-    at_scale = ((int64_t)tile * a.groups * chunks + r / 128) * 512 + (r % 32) * 16 +
-               (r % 128) / 32 * 4;
-    step_scale = chunks * 512;
+    words = a.tile_words;
+    at_scale = (int64_t)tile * a.tile_bytes + r * words * 4;
+    step = a.tile_rows * words * 4;
   } else {
+    words = 1;
     at_scale = row * a.ld_scales;
-    step_scale = 4;
+    step = 4;
   }
   uint8_t* codes = a.codes + row * a.ld_codes;
   const int code_cols = (a.d + 31) / 32 * 32;
@@ -120,27 +120,29 @@ quant_kernel(const Mx4Quant a) {
         const int unit = turn * kSpan + i * TPR + t, col = unit * 8;
         if (p > 0) amax[i] = block_amax<FMT>(v[i]);
         const bool bad = amax[i] >= kInfBits;
-        float step = 0.f;
+        float unit_step = 0.f;
         uint32_t s = 0, c = 0;
         if (bad) {
           s = Mx4<FMT>::kNanScale;
         } else if (col / Mx4<FMT>::kBlock * Mx4<FMT>::kBlock < a.d) {
-          s = mx4_scale<FMT>(amax[i], row_exp, &step);
-          c = mx4_codes<FMT>(v[i], step);
+          s = mx4_scale<FMT>(amax[i], row_exp, &unit_step);
+          c = mx4_codes<FMT>(v[i], unit_step);
         }
         if (col < code_cols) *reinterpret_cast<uint32_t*>(codes + p * a.plane_codes + unit * 4) = c;
         // four scales to a word, stored by the lane that holds the first
         constexpr int kLanes = Mx4<FMT>::kBlock / 8;
         s |= __shfl_down_sync(0xFFFFFFFFu, s, kLanes) << 8;
         s |= __shfl_down_sync(0xFFFFFFFFu, s, 2 * kLanes) << 16;
-        if (lane % (4 * kLanes) == 0 && col < a.scale_cols)
+        if (lane % (4 * kLanes) == 0 && col < a.scale_cols) {
+          const int w = unit / (4 * kLanes);
           *reinterpret_cast<uint32_t*>(a.scales + p * a.plane_scales + at_scale +
-                                       (int64_t)(unit / (4 * kLanes)) * step_scale) = s;
+                                       w / words * step + w % words * 4) = s;
+        }
         if (p + 1 < a.planes && !bad) {
           float q[8];
           e2m1x8_to_float(c, q);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] = __fmaf_rn(-q[j], step, v[i][j]);   // exact
+          for (int j = 0; j < 8; ++j) v[i][j] = __fmaf_rn(-q[j], unit_step, v[i][j]);   // exact
         }
       }
     }

@@ -322,7 +322,9 @@ struct Mx4Quant {
   int planes;               // terms; 1 in the table form
   // operand form
   int64_t plane_codes, plane_scales;    // bytes between terms
-  int tile_rows, groups;    // rows of a tile, 4-byte scale groups of a row
+  int tile_rows;            // rows of a tile; its scales are [stage][tile_rows][tile_words]
+  int tile_words;           // 4-byte words, tile_bytes in all
+  int64_t tile_bytes;
   int aligned;              // set by the launch: rows start on 16 bytes
 };
 cudaError_t launch_mx4_quant(Mx4Quant a, int fmt, int x_type, bool operand, cudaStream_t st);
