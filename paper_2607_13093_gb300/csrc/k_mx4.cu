@@ -4,11 +4,14 @@
 // terms, each the 4-bit form of what the terms before it left over.
 //
 // Bound by memory: an element is read once (2 or 4 bytes) and leaves 4.5 or
-// 4.25 bits.  A row belongs to a warp or a block, whose threads hold it in
-// registers, 8 consecutive columns a thread and step, while the row's and the
-// blocks' maxima are made (a block's by one or two shuffles); rows too long for
-// the registers are read twice.
+// 4.25 bits.  A row belongs to a warp or a block, whose threads hold it as it was
+// read, 16 consecutive columns a thread and step, while the row's and the blocks'
+// maxima are made; rows too long for the registers are read twice.  What a
+// block's scale costs is shared by its 16 columns (with 8 columns a thread,
+// 32000 x 4096 bf16 rows took 125 us).
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "mx4.cuh"
 #include "sm100_ptx.cuh"
@@ -17,64 +20,124 @@
 namespace sph {
 namespace {
 
-constexpr int kQuantUnits = 4;      // 8-column steps a thread holds in registers
+constexpr int kCols = 16;           // columns of a thread and step
 
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-
-// Columns col .. col + 7 of a row of d columns; zeros beyond it.  vec: the row
-// starts on 16 bytes.  Coherent loads: the caller's kernel may have written x
-// just before.
+// 16 columns as they lie in memory.
 template <class T>
-__device__ __forceinline__ void load8(const T* row, int col, int d, bool vec, float (&v)[8]) {
-  if (vec && col + 8 <= d) {
-    uint4 w[sizeof(T) / 2];
+struct Raw {
+  uint4 w[sizeof(T)];
+};
+template <class T> __device__ __forceinline__ float element(const Raw<T>& r, int j);
+template <> __device__ __forceinline__ float element<float>(const Raw<float>& r, int j) {
+  return reinterpret_cast<const float*>(r.w)[j];
+}
+template <> __device__ __forceinline__ float element<__half>(const Raw<__half>& r, int j) {
+  return __half2float(reinterpret_cast<const __half*>(r.w)[j]);
+}
+template <> __device__ __forceinline__ float element<__nv_bfloat16>(const Raw<__nv_bfloat16>& r,
+                                                                     int j) {
+  const uint32_t w = reinterpret_cast<const uint32_t*>(r.w)[j / 2];
+  return __uint_as_float(j % 2 ? w & 0xFFFF0000u : w << 16);
+}
+
+// Columns col .. col + 15 of each lane's row part (a warp's lanes hold 512
+// consecutive columns of one row); zeros past column d.  aligned: the row starts on
+// 16 bytes.  Other rows go through the warp's piece of shared memory, so that
+// neighbouring lanes read neighbouring columns.  Coherent loads: the caller's
+// kernel may have written x just before.
+template <class T>
+__device__ __forceinline__ void load_raw(const T* row, int col, int d, bool aligned, T* stage,
+                                         int lane, Raw<T>& r) {
+  if (aligned && col + kCols <= d) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-      w[i] = reinterpret_cast<const uint4*>(row + col)[i];
-    const T* e = reinterpret_cast<const T*>(w);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
+    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = reinterpret_cast<const uint4*>(row + col)[i];
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = col + j < d ? to_f32(row[col + j]) : 0.f;
+    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = make_uint4(0, 0, 0, 0);
+    if (aligned) {
+      T* e = reinterpret_cast<T*>(r.w);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        if (col + j < d) e[j] = row[col + j];
+    }
+  }
+  if (!aligned) {
+    // lane l's 16 columns start at 18 l (17 l for fp32): no two lanes in one bank
+    constexpr int kPitch = kCols + (sizeof(T) == 4 ? 1 : 2);
+    const int first = col - lane * kCols;
+    T v[kCols];
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) {
+      const int c = j * 32 + lane;
+      v[j] = first + c < d ? row[first + c] : T(0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) {
+      const int c = j * 32 + lane;
+      stage[c / kCols * kPitch + c % kCols] = v[j];
+    }
+    __syncwarp();
+    T* e = reinterpret_cast<T*>(r.w);
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) e[j] = stage[lane * kPitch + j];
+    __syncwarp();
   }
 }
 
-// Bits of the largest magnitude of a block, from its threads' eights.
+// Bits of the largest magnitude of a block as fp32 (kInfBits or more: it holds a
+// NaN or an infinity).  16-bit types compare two columns an instruction, as bits.
+template <int FMT, class T>
+__device__ __forceinline__ unsigned block_amax(const Raw<T>& r) {
+  unsigned m = 0;
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(r.w);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) m = max(m, w[j] & 0x7FFFFFFFu);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kCols / 2; ++j) m = __vmaxu2(m, w[j] & 0x7FFF7FFFu);
+    m = max(m >> 16, m & 0xFFFFu);
+  }
+  if constexpr (FMT == MX4_E8M0) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) m <<= 16;
+  if constexpr (std::is_same<T, __half>::value)
+    m = m >= 0x7C00u ? kInfBits : __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+  return m;
+}
 template <int FMT>
-__device__ __forceinline__ unsigned block_amax(const float (&v)[8]) {
+__device__ __forceinline__ unsigned block_amax(const float (&v)[kCols]) {
   unsigned m = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-  m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-  if constexpr (FMT == MX4_E8M0) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+  for (int j = 0; j < kCols; ++j) m = max(m, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+  if constexpr (FMT == MX4_E8M0) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
   return m;
 }
 
-// TPR threads a row.  OPERAND: the product's form.
-template <class T, int FMT, int TPR, bool OPERAND>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
-quant_kernel(const Mx4Quant a) {
-  constexpr int kRows = TPR < 128 ? 128 / TPR : 1;     // rows of a block
-  constexpr int kSpan = TPR * kQuantUnits;             // 8-column steps a turn
+// TPR threads a row, U steps of 16 columns a thread and turn.  OPERAND: the
+// product's form.
+template <class T, int FMT, int TPR, int U, bool OPERAND>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) quant_kernel(const Mx4Quant a) {
+  constexpr int kThreads = TPR < 128 ? 128 : TPR;
+  constexpr int kRows = kThreads / TPR;                // rows of a block
+  constexpr int kSpan = TPR * U;                       // steps a turn
+  __shared__ T s_stage[kThreads / 32][32 * (kCols + 2)];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (row >= a.rows) return;                           // (whole warps; TPR >= 128: whole blocks)
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  const bool vec = a.aligned != 0;
-  const int turns = (a.scale_cols / 8 + kSpan - 1) / kSpan;
-  float v[kQuantUnits][8];
-  unsigned amax[kQuantUnits];
+  T* stage = s_stage[threadIdx.x / 32];
+  const bool aligned = a.aligned != 0;
+  const int turns = (a.scale_cols / kCols + kSpan - 1) / kSpan;
+  Raw<T> raw[U];
+  unsigned amax[U];
   auto load = [&](int turn) {
 #pragma unroll
-    for (int i = 0; i < kQuantUnits; ++i)
-      load8(x, (turn * kSpan + i * TPR + t) * 8, a.d, vec, v[i]);
+    for (int i = 0; i < U; ++i)
+      load_raw<T>(x, (turn * kSpan + i * TPR + t) * kCols, a.d, aligned, stage, lane, raw[i]);
 #pragma unroll
-    for (int i = 0; i < kQuantUnits; ++i) amax[i] = block_amax<FMT>(v[i]);
+    for (int i = 0; i < U; ++i) amax[i] = block_amax<FMT>(raw[i]);
   };
   int row_exp = 0;
   if constexpr (FMT == MX4_E4M3) {
@@ -82,7 +145,7 @@ quant_kernel(const Mx4Quant a) {
     for (int turn = 0; turn < turns; ++turn) {
       load(turn);
 #pragma unroll
-      for (int i = 0; i < kQuantUnits; ++i)
+      for (int i = 0; i < U; ++i)
         if (amax[i] < kInfBits) top = max(top, amax[i]);
     }
     top = __reduce_max_sync(0xFFFFFFFFu, top);
@@ -96,8 +159,8 @@ quant_kernel(const Mx4Quant a) {
     row_exp = mx4_row_exp(top);
   }
   if (t == 0 && a.row_scale) a.row_scale[row] = exp2_int(row_exp);
-  // the row's scale words: word i at at_scale + i / tile_words * step + i % tile_words
-  // words (table form: one after another)
+  // the row's scale words: word i at at_scale + i / words * step + i % words * 4
+  // (table form: one after another)
   int64_t at_scale, step;
   int words;
   if constexpr (OPERAND) {
@@ -114,59 +177,73 @@ quant_kernel(const Mx4Quant a) {
   const int code_cols = (a.d + 31) / 32 * 32;
   for (int turn = 0; turn < turns; ++turn) {
     if (FMT == MX4_E8M0 || turns > 1) load(turn);
-    for (int p = 0; p < a.planes; ++p) {
 #pragma unroll
-      for (int i = 0; i < kQuantUnits; ++i) {
-        const int unit = turn * kSpan + i * TPR + t, col = unit * 8;
-        if (p > 0) amax[i] = block_amax<FMT>(v[i]);
+    for (int i = 0; i < U; ++i) {
+      const int unit = turn * kSpan + i * TPR + t, col = unit * kCols;
+      float v[kCols];
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) v[j] = element<T>(raw[i], j);
+      for (int p = 0; p < (OPERAND ? a.planes : 1); ++p) {
+        if (p > 0) amax[i] = block_amax<FMT>(v);
         const bool bad = amax[i] >= kInfBits;
         float unit_step = 0.f;
-        uint32_t s = 0, c = 0;
+        uint32_t s = 0, c[kCols / 8] = {0, 0};
         if (bad) {
           s = Mx4<FMT>::kNanScale;
         } else if (col / Mx4<FMT>::kBlock * Mx4<FMT>::kBlock < a.d) {
           s = mx4_scale<FMT>(amax[i], row_exp, &unit_step);
-          c = mx4_codes<FMT>(v[i], unit_step);
+          mx4_codes<FMT>(v, unit_step, c);
         }
-        if (col < code_cols) *reinterpret_cast<uint32_t*>(codes + p * a.plane_codes + unit * 4) = c;
+        if (col < code_cols)
+          *reinterpret_cast<uint2*>(codes + (OPERAND ? p * a.plane_codes : 0) + unit * (kCols / 2)) =
+              make_uint2(c[0], c[1]);
         // four scales to a word, stored by the lane that holds the first
-        constexpr int kLanes = Mx4<FMT>::kBlock / 8;
+        constexpr int kLanes = Mx4<FMT>::kBlock / kCols;
         s |= __shfl_down_sync(0xFFFFFFFFu, s, kLanes) << 8;
         s |= __shfl_down_sync(0xFFFFFFFFu, s, 2 * kLanes) << 16;
         if (lane % (4 * kLanes) == 0 && col < a.scale_cols) {
           const int w = unit / (4 * kLanes);
-          *reinterpret_cast<uint32_t*>(a.scales + p * a.plane_scales + at_scale +
+          *reinterpret_cast<uint32_t*>(a.scales + (OPERAND ? p * a.plane_scales : 0) + at_scale +
                                        w / words * step + w % words * 4) = s;
         }
-        if (p + 1 < a.planes && !bad) {
-          float q[8];
-          e2m1x8_to_float(c, q);
+        if (OPERAND && p + 1 < a.planes && !bad) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] = __fmaf_rn(-q[j], unit_step, v[i][j]);   // exact
+          for (int h = 0; h < kCols / 8; ++h) {
+            float q[8];
+            e2m1x8_to_float(c[h], q);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 * h + j] = __fmaf_rn(-q[j], unit_step, v[8 * h + j]);  // exact
+          }
         }
       }
     }
   }
 }
 
-template <class T, int FMT, bool OPERAND>
+template <class T, int FMT, int TPR, int U, bool OPERAND>
 cudaError_t launch(const Mx4Quant& a, cudaStream_t st) {
-  // one warp a row up to 1024 columns, a block of 128 threads up to 4096, of
-  // 256 above: each holds its row in registers up to 8192 columns.
-  if (a.scale_cols <= 32 * kQuantUnits * 8)
-    return launch_pdl(quant_kernel<T, FMT, 32, OPERAND>, dim3((unsigned)((a.rows + 3) / 4)),
-                      dim3(128), 0, st, a);
-  if (a.scale_cols <= 128 * kQuantUnits * 8)
-    return launch_pdl(quant_kernel<T, FMT, 128, OPERAND>, dim3((unsigned)a.rows), dim3(128), 0, st,
-                      a);
-  return launch_pdl(quant_kernel<T, FMT, 256, OPERAND>, dim3((unsigned)a.rows), dim3(256), 0, st,
-                    a);
+  constexpr int kThreads = TPR < 128 ? 128 : TPR, kRows = kThreads / TPR;
+  return launch_pdl(quant_kernel<T, FMT, TPR, U, OPERAND>,
+                    dim3((unsigned)((a.rows + kRows - 1) / kRows)), dim3(kThreads), 0, st, a);
+}
+// Hidden states are few, and the product waits for them: one step a thread and as
+// many threads as a row has, up to 512.  A table's rows are many: two steps a
+// thread, a warp a row up to 1024 columns, a block of 128 threads up to 4096, of 256
+// above; each holds its row in registers up to 8192 columns.
+template <class T, int FMT>
+cudaError_t launch_f(const Mx4Quant& a, bool operand, cudaStream_t st) {
+  if (operand) {
+    if (a.scale_cols <= 128 * kCols) return launch<T, FMT, 128, 1, true>(a, st);
+    return launch<T, FMT, 512, 1, true>(a, st);
+  }
+  if (a.scale_cols <= 32 * 2 * kCols) return launch<T, FMT, 32, 2, false>(a, st);
+  if (a.scale_cols <= 128 * 2 * kCols) return launch<T, FMT, 128, 2, false>(a, st);
+  return launch<T, FMT, 256, 2, false>(a, st);
 }
 template <class T>
 cudaError_t launch_t(const Mx4Quant& a, int fmt, bool operand, cudaStream_t st) {
-  if (fmt == MX4_E4M3)
-    return operand ? launch<T, MX4_E4M3, true>(a, st) : launch<T, MX4_E4M3, false>(a, st);
-  return operand ? launch<T, MX4_E8M0, true>(a, st) : launch<T, MX4_E8M0, false>(a, st);
+  return fmt == MX4_E4M3 ? launch_f<T, MX4_E4M3>(a, operand, st)
+                         : launch_f<T, MX4_E8M0>(a, operand, st);
 }
 
 }  // namespace

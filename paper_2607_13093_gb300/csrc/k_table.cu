@@ -102,42 +102,49 @@ __device__ __forceinline__ void table_cols(const Lookup& a, int64_t id, int col,
   }
 }
 
-// TB tokens and kLookSpan columns a block; the tokens' rows are requested together.
-template <class TT, int FMT, class OT, bool VEC, int TB>
+// A block takes one token and `turns` spans of kLookSpan columns, U of them requested
+// together.
+template <class TT, int FMT, class OT, bool VEC, int U>
 __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const Lookup a) {
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const int span = (int)(blockIdx.x % a.spans);
-  const int64_t t0 = (int64_t)(blockIdx.x / a.spans) * TB;
-  const int col = span * kLookSpan + (VEC ? (int)threadIdx.x * 8 : (int)threadIdx.x);
-  float v[TB][8];
+  const int64_t t = blockIdx.x / a.blocks;
+  const int first = (int)(blockIdx.x % a.blocks) * a.turns * kLookSpan +
+                    (VEC ? (int)threadIdx.x * 8 : (int)threadIdx.x);
+  const int64_t id = a.tokens ? a.tokens[t] : t;
+  const bool there = id >= 0 && id < a.V;
+  if (!there && id != a.padding && first == 0) atomicOr(a.status, ERR_BAD_INDEX);
+  OT* out = static_cast<OT*>(a.out) + t * a.ld_out;
+  for (int n = 0; n < a.turns; n += U) {
+    float v[U][8];
 #pragma unroll
-  for (int i = 0; i < TB; ++i) {
+    for (int i = 0; i < U; ++i) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-    if (t0 + i >= a.n) continue;
-    const int64_t id = a.tokens ? a.tokens[t0 + i] : t0 + i;
-    if (id >= 0 && id < a.V) table_cols<TT, FMT, VEC>(a, id, col, v[i]);
-    else if (id != a.padding && col == 0) atomicOr(a.status, ERR_BAD_INDEX);
-  }
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+      const int col = first + (n + i) * kLookSpan;
+      if (there && n + i < a.turns && col < a.d) table_cols<TT, FMT, VEC>(a, id, col, v[i]);
+    }
 #pragma unroll
-  for (int i = 0; i < TB; ++i) {
-    if (t0 + i >= a.n) break;
+    for (int i = 0; i < U; ++i) {
+      const int col = first + (n + i) * kLookSpan;
+      if (n + i >= a.turns || col >= a.d) break;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] *= a.scale;
-    store_cols<OT, VEC>(static_cast<OT*>(a.out) + (t0 + i) * a.ld_out, col, kLookThreads, a.d, v[i]);
+      for (int j = 0; j < 8; ++j) v[i][j] *= a.scale;
+      store_cols<OT, VEC>(out, col, kLookThreads, a.d, v[i]);
+    }
   }
 }
 
 template <class TT, int FMT, class OT, bool VEC>
-cudaError_t launch_lookup_v(const Lookup& a, int sm_count, cudaStream_t st) {
-  // four tokens a block once that still leaves every SM eight blocks
-  const int64_t blocks = a.n * a.spans;
-  if (blocks >= (int64_t)sm_count * 32)
-    return launch_pdl(lookup_kernel<TT, FMT, OT, VEC, 4>,
-                      dim3((unsigned)((a.n + 3) / 4 * a.spans)), dim3(kLookThreads), 0, st, a);
-  return launch_pdl(lookup_kernel<TT, FMT, OT, VEC, 1>, dim3((unsigned)blocks), dim3(kLookThreads),
-                    0, st, a);
+cudaError_t launch_lookup_v(Lookup a, int sm_count, cudaStream_t st) {
+  // one block a token once that gives every SM sixteen, else a block for each span
+  const int spans = (a.d + kLookSpan - 1) / kLookSpan;
+  a.turns = a.n >= (int64_t)sm_count * 16 ? spans : 1;
+  a.blocks = (spans + a.turns - 1) / a.turns;
+  const dim3 grid((unsigned)(a.n * a.blocks));
+  if (a.turns > 1)
+    return launch_pdl(lookup_kernel<TT, FMT, OT, VEC, 4>, grid, dim3(kLookThreads), 0, st, a);
+  return launch_pdl(lookup_kernel<TT, FMT, OT, VEC, 1>, grid, dim3(kLookThreads), 0, st, a);
 }
 template <class TT, int FMT, class OT>
 cudaError_t launch_lookup_o(const Lookup& a, bool vec, int sm_count, cudaStream_t st) {
@@ -159,23 +166,27 @@ int type_size(int t) { return t == TAB_FP32 ? 4 : 2; }
 // ---------------------------------------------------------------------------
 // gradient: the sort
 // ---------------------------------------------------------------------------
-constexpr int kSortThreads = 1024, kSortItems = 4, kSortTile = kSortThreads * kSortItems;
+constexpr int kSortThreads = 512, kSortItems = 16, kSortTile = kSortThreads * kSortItems;
 constexpr int kSortBits = 9, kSortBins = 1 << kSortBits, kSortWarps = kSortThreads / 32;
 
 struct SortSmem {
   uint32_t hist[kSortBins];       // this CTA's count of each digit (read by the cluster)
   uint32_t base[kSortBins];       // where its next element of a digit goes
-  uint32_t tile[kSortBins];       // the same at the start of the current tile
-  uint32_t part[kSortBins / 32];
+  uint32_t part[kSortWarps];
   uint16_t warp[kSortWarps][kSortBins];
+  int32_t key[kSortTile];         // a sort of one tile stays here between passes
+  int32_t pos[kSortTile];
 };
 
-// One cluster sorts: stable radix passes of 9 bits over (id, position), each CTA a
-// contiguous part.  A pass counts digits per CTA, reads the counts of the
-// cluster's CTAs through distributed shared memory, and moves its part tile by
-// tile; within a tile, equal digits of a warp are ranked by match.any, warps by a
-// prefix over their counts.  Ids out of range become V, which sorts last.
-__global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, int parts, int passes) {
+// One cluster sorts: stable radix passes over (id, position) with digits of at most
+// 9 bits, each CTA a contiguous part.  A warp's items are consecutive; equal
+// digits within a warp are ranked by match.any, its warps by a prefix over their
+// counts, the CTAs by one over theirs, read through distributed shared memory.
+// Up to kSortTile tokens (one CTA) the passes stay in shared memory; parts of one
+// tile get their counts from the ranking, longer ones from a pass of their own.
+// Ids out of range become V, which sorts last.
+__global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, int parts, int passes,
+                                                            int bits) {
   extern __shared__ __align__(16) uint8_t sort_raw[];
   SortSmem& s = *reinterpret_cast<SortSmem*>(sort_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -184,69 +195,80 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
   ptx::griddep_launch_dependents();
   const int part = (a.n + parts - 1) / parts;
   const int p0 = min(a.n, rank * part), p1 = min(a.n, p0 + part);
+  const bool one = part <= kSortTile, local = parts == 1 && one;
+  const int bins = 1 << bits;
   for (int pass = 0; pass < passes; ++pass) {
-    const int shift = pass * kSortBits;
+    const int shift = pass * bits;
     // passes end in buffer 0: the last one writes it
     const int to = (passes - 1 - pass) & 1;
-    const int32_t* src_k = a.keys[to ^ 1];
-    const int32_t* src_p = a.pos[to ^ 1];
-    int32_t* dst_k = a.keys[to];
-    int32_t* dst_p = a.pos[to];
+    const bool last = pass == passes - 1;
     auto key_of = [&](int i) {
-      if (pass > 0) return __ldcg(src_k + i);
+      if (pass > 0) return local ? s.key[i] : __ldcg(a.keys[to ^ 1] + i);
       const int32_t id = a.tokens[i];
       return id >= 0 && id < a.V ? id : a.V;
     };
-    auto digit = [&](int32_t k) { return (int)((uint32_t)k >> shift) & (kSortBins - 1); };
-    for (int b = tid; b < kSortBins; b += kSortThreads) s.hist[b] = 0;
-    __syncthreads();
-    for (int i = p0 + tid; i < p1; i += kSortThreads) {
-      if (pass == 0) {
-        const int32_t id = a.tokens[i];
-        if ((id < 0 || id >= a.V) && id != a.padding) atomicOr(a.status, ERR_BAD_INDEX);
+    auto digit = [&](int32_t k) { return (int)((uint32_t)k >> shift) & (bins - 1); };
+    // Where each digit's elements of this CTA start, from its own counts (thread b:
+    // digit b).
+    auto place = [&](uint32_t mine) {
+      uint32_t total = mine, below = 0;
+      if (parts > 1) {
+        s.hist[tid] = mine;
+        ptx::cluster_sync();
+        total = 0;
+        for (int c = 0; c < parts; ++c) {
+          uint32_t h;
+          asm volatile("ld.shared::cluster.u32 %0, [%1];"
+                       : "=r"(h)
+                       : "r"(ptx::mapa(ptx::smem_u32(&s.hist[tid]), (uint32_t)c))
+                       : "memory");
+          if (c < rank) below += h;
+          total += h;
+        }
       }
-      atomicAdd(&s.hist[digit(key_of(i))], 1u);
-    }
-    ptx::cluster_sync();
-    uint32_t total = 0, below = 0;
-    if (tid < kSortBins) {
-      for (int c = 0; c < parts; ++c) {
-        uint32_t h;
-        asm volatile("ld.shared::cluster.u32 %0, [%1];"
-                     : "=r"(h)
-                     : "r"(ptx::mapa(ptx::smem_u32(&s.hist[tid]), (uint32_t)c))
-                     : "memory");
-        if (c < rank) below += h;
-        total += h;
-      }
-    }
-    uint32_t incl = total;
+      uint32_t incl = total;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-      if (lane >= o) incl += up;
-    }
-    if (tid < kSortBins && lane == 31) s.part[warp] = incl;
-    __syncthreads();
-    if (tid < kSortBins) {
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      if (lane == 31) s.part[warp] = incl;
+      __syncthreads();
       uint32_t before = 0;
       for (int w = 0; w < warp; ++w) before += s.part[w];
       s.base[tid] = before + incl - total + below;
+      __syncthreads();
+    };
+    if (!one) {
+      s.base[tid] = 0;
+      __syncthreads();
+      for (int i = p0 + tid; i < p1; i += kSortThreads) atomicAdd(&s.base[digit(key_of(i))], 1u);
+      __syncthreads();
+      const uint32_t mine = s.base[tid];
+      __syncthreads();
+      place(mine);
     }
-    for (int t0 = p0; t0 < p1; t0 += kSortTile) {
+    for (int t0 = p0; t0 < p1 || (one && t0 == p0); t0 += kSortTile) {
+      // items of a thread: enough for the tile, so that short lists take few rounds
+      const int count = min(kSortTile, p1 - t0), rounds = (count + kSortThreads - 1) / kSortThreads;
       int32_t k[kSortItems], p[kSortItems];
       uint32_t r[kSortItems];
+      const int first = t0 + warp * 32 * rounds + lane;
 #pragma unroll
       for (int i = 0; i < kSortItems; ++i) {
-        const int at = t0 + warp * (32 * kSortItems) + i * 32 + lane;
-        k[i] = at < p1 ? key_of(at) : 0;
-        p[i] = at < p1 ? (pass == 0 ? at : __ldcg(src_p + at)) : -1;
+        if (i >= rounds) break;
+        const int at = first + i * 32;
+        const bool in = at < t0 + count;
+        k[i] = in ? key_of(at) : 0;
+        p[i] = !in ? -1 : pass == 0 ? at : local ? s.pos[at] : __ldcg(a.pos[to ^ 1] + at);
+        if (pass == 0 && in && k[i] == a.V && a.tokens[at] != a.padding)
+          atomicOr(a.status, ERR_BAD_INDEX);
       }
-      for (int b = lane; b < kSortBins / 2; b += 32)
-        reinterpret_cast<uint32_t*>(s.warp[warp])[b] = 0;
+      for (int b = lane; b < bins / 2; b += 32) reinterpret_cast<uint32_t*>(s.warp[warp])[b] = 0;
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < kSortItems; ++i) {
+        if (i >= rounds) break;
         const unsigned live = __ballot_sync(0xFFFFFFFFu, p[i] >= 0);
         if (p[i] >= 0) {
           const int dg = digit(k[i]);
@@ -259,32 +281,41 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
         __syncwarp();
       }
       __syncthreads();
-      if (tid < kSortBins) {
-        uint32_t run = 0;
-#pragma unroll 8
+      uint32_t run = 0;
+      if (tid < bins) {
+#pragma unroll
         for (int w = 0; w < kSortWarps; ++w) {
           const uint32_t c = s.warp[w][tid];
           s.warp[w][tid] = (uint16_t)run;
           run += c;
         }
-        s.tile[tid] = s.base[tid];
-        s.base[tid] += run;
       }
-      __syncthreads();
+      if (one) place(run);
+      else __syncthreads();
 #pragma unroll
       for (int i = 0; i < kSortItems; ++i) {
+        if (i >= rounds) break;
         if (p[i] >= 0) {
           const int dg = digit(k[i]);
-          const uint32_t to_at = s.tile[dg] + s.warp[warp][dg] + r[i];
-          dst_k[to_at] = k[i];
-          dst_p[to_at] = p[i];
+          const uint32_t at = s.base[dg] + s.warp[warp][dg] + r[i];
+          if (local && !last) {
+            s.key[at] = k[i];
+            s.pos[at] = p[i];
+          } else {
+            a.keys[to][at] = k[i];
+            a.pos[to][at] = p[i];
+          }
         }
       }
       __syncthreads();
+      if (!one) {
+        s.base[tid] += run;
+        __syncthreads();
+      }
     }
     // the pass's writes reach the cluster's other CTAs, and none still reads
-    // this one's counts when the next pass clears them
-    ptx::cluster_sync();
+    // this one's counts when the next pass writes them
+    if (parts > 1) ptx::cluster_sync();
   }
 }
 
@@ -340,7 +371,8 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const TableGrad a, i
 // gradient: sums over ranges of sorted positions, and the join
 // ---------------------------------------------------------------------------
 constexpr int kSumThreads = 128;
-constexpr int kSumBatch = 8;        // rows requested together (4 where columns are scattered)
+constexpr int kSumBytes = 256;      // shared memory of a thread: rows requested ahead
+constexpr int kShortRun = 32;       // positions of a run that one range takes whole
 
 // Columns of thread `u` of `ct` in column group g.
 template <bool VEC>
@@ -364,31 +396,61 @@ __device__ __forceinline__ void write_row(const TableGrad& a, int32_t id, int co
   store_cols<OT, VEC>(row, col, ct, a.d, v);
 }
 
+// The part of a run of equal ids around the boundary before position `at` (whose key
+// `id` is also that of at - 1): its start and end, exact for runs of at most
+// kShortRun positions; longer ones give more than kShortRun.
+__device__ __forceinline__ void run_around(const int32_t* keys, int n, int at, int32_t id, int* s,
+                                           int* e) {
+  int b = at - 1, f = at + 1;
+  while (b > 0 && at - b <= kShortRun && keys[b - 1] == id) --b;
+  while (f < n && f - b <= kShortRun && keys[f] == id) ++f;
+  *s = b;
+  *e = f;
+}
+
 // ct threads a range of a.range sorted positions and 8 ct columns (128 / ct
-// ranges a block).  A run of equal ids inside the range is written out; the part of
-// one that began before the range goes to slot 2 r of the partial sums, that of
-// one that begins in it and goes on to slot 2 r + 1.
+// ranges a block).  A run of equal ids of at most kShortRun positions is summed by
+// the range that it begins in and written out; of a longer one each range sums its
+// own part, into slot 2 r of the partial sums where the run began earlier, into
+// slot 2 r + 1 where it begins in the range and goes on (written out where it
+// does neither).  A thread's columns of the next rows are on their way to its own
+// piece of shared memory while it adds: nothing is shared between threads.  (With
+// rows in registers the code for a run's end stood once for each of them:
+// 32768 rows x 4096 bf16 159 us.)
 template <class T, class OT, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int ct) {
+  __shared__ uint4 s_rows[kSumBytes / 16][kSumThreads];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int u = threadIdx.x % ct;
   const int group = (int)(blockIdx.x % a.groups);
   const int64_t r = (int64_t)(blockIdx.x / a.groups) * (kSumThreads / ct) + threadIdx.x / ct;
-  const int64_t i0 = r * a.range;
   const int col = sum_col<VEC>(group, u, ct);
-  if (i0 >= a.n || col >= a.d) return;
-  const int i1 = (int)min((int64_t)a.n, i0 + a.range);
+  if (r * a.range >= a.n || col >= a.d) return;
+  const int i0 = (int)(r * a.range), i1 = min(a.n, i0 + a.range);
   const int32_t* keys = a.keys[0];
   const int32_t* pos = a.pos[0];
+  int begin = i0, end = i1;
+  bool open_left = false, open_right = false;
+  if (i0 > 0 && keys[i0 - 1] == keys[i0]) {
+    int s, e;
+    run_around(keys, a.n, i0, keys[i0], &s, &e);
+    if (e - s > kShortRun) open_left = true;
+    else begin = e;
+  }
+  if (begin >= i1) return;
+  if (i1 < a.n && keys[i1 - 1] == keys[i1]) {
+    int s, e;
+    run_around(keys, a.n, i1, keys[i1], &s, &e);
+    if (e - s > kShortRun) open_right = true;
+    else end = e;
+  }
   float acc[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-  int32_t cur = keys[i0];
-  bool open_left = i0 > 0 && keys[i0 - 1] == cur;
-  auto flush = [&](bool open_right) {
-    if (cur == a.V) return;
-    if (!open_left && !open_right) {
+  int32_t cur = keys[begin];
+  auto flush = [&](bool right) {
+    if (!open_left && !right) {
       write_row<OT, VEC>(a, cur, col, ct, acc);
     } else {
       float* p = a.partial + (2 * r + (open_left ? 0 : 1)) * a.ld_partial + group * ct * 8 + u * 8;
@@ -396,40 +458,99 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
       reinterpret_cast<float4*>(p)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
     }
   };
-  constexpr int kBatch = VEC ? kSumBatch : kSumBatch / 2;
-  for (int b = (int)i0; b < i1; b += kBatch) {
-    int32_t k[kBatch];
-    float x[kBatch][8];
+  auto add = [&](int32_t k, const float (&x)[8]) {
+    if (k != cur) {
+      flush(false);
+      cur = k;
+      open_left = false;
 #pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
-      k[q] = b + q < i1 ? keys[b + q] : a.V;
-      if (k[q] < a.V)
-        load_cols<T, VEC>(static_cast<const T*>(a.d_out) + (int64_t)pos[b + q] * a.ld_d_out, col, ct,
-                          a.d, x[q]);
+      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
     }
 #pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
-      if (b + q >= i1) break;
-      if (k[q] != cur) {
-        flush(false);
-        cur = k[q];
-        open_left = false;
+    for (int j = 0; j < 8; ++j) acc[j] += x[j];
+  };
+  // (ids without a row of their own sort last)
+  while (end > begin && keys[end - 1] == a.V) {
+    // a whole range of them, or its tail: they end the list, so halve towards the first
+    int lo = begin, hi = end - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (keys[mid] == a.V) hi = mid;
+      else lo = mid + 1;
+    }
+    end = lo;
+    open_right = false;
+  }
+  if (end == begin) return;
+  auto row_of = [&](int i) { return static_cast<const T*>(a.d_out) + (int64_t)pos[i] * a.ld_d_out; };
+  if constexpr (VEC) {
+    constexpr int kPieces = (int)sizeof(T) / 2, kAhead = kSumBytes / 16 / kPieces;
+    auto request = [&](int i) {
+      if (i < end) {
+        const T* row = row_of(i) + col;
+        const int slot = (i - begin) % kAhead * kPieces;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        for (int q = 0; q < kPieces; ++q) {
+          // columns past the row's last are zeros, and not read
+          const int bytes = min(16, max(0, (a.d - col) * (int)sizeof(T) - 16 * q));
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                           ptx::smem_u32(&s_rows[slot + q][threadIdx.x])),
+                       "l"(bytes > 0 ? reinterpret_cast<const uint4*>(row) + q
+                                     : reinterpret_cast<const uint4*>(row)),
+                       "r"(bytes)
+                       : "memory");
+        }
       }
-      if (k[q] < a.V) {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] += x[q][j];
+    for (int i = 0; i < kAhead - 1; ++i) request(begin + i);
+    for (int i = begin; i < end; ++i) {
+      request(i + kAhead - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+      uint4 w[kPieces];
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q)
+        w[q] = s_rows[(i - begin) % kAhead * kPieces + q][threadIdx.x];
+      const T* e = reinterpret_cast<const T*>(w);
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = to_f32(e[j]);
+      add(keys[i], x);
+    }
+  } else {
+    constexpr int kAhead = kSumBytes / 32;
+    for (int b = begin; b < end; b += kAhead) {
+      const int m = min(kAhead, end - b);
+#pragma unroll
+      for (int h = 0; h < kAhead; h += 4) {
+        float x[4][8];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (h + q < m) load_cols<T, false>(row_of(b + h + q), col, ct, a.d, x[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (h + q < m) {
+            s_rows[2 * (h + q)][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][0]);
+            s_rows[2 * (h + q) + 1][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][4]);
+          }
+      }
+      for (int q = 0; q < m; ++q) {
+        const uint4 lo = s_rows[2 * q][threadIdx.x], hi = s_rows[2 * q + 1][threadIdx.x];
+        const float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z),
+                            __uint_as_float(lo.w), __uint_as_float(hi.x), __uint_as_float(hi.y),
+                            __uint_as_float(hi.z), __uint_as_float(hi.w)};
+        add(keys[b + q], x);
       }
     }
   }
-  flush(i1 < a.n && keys[i1] == cur);
+  flush(open_right);
 }
 
 constexpr int kJoinThreads = 256;
 
-// A block for each range and column group; it goes on only where a run begins in
-// the range and crosses its end.  The run's parts (slot 2 r + 1, then slot 2 j of
+// A block for each range and column group; it goes on only where a run of more than
+// kShortRun positions begins in the range and crosses its end.  The run's parts (slot 2 r + 1, then slot 2 j of
 // the ranges j it reaches) are shared by the block's thread groups in contiguous
 // shares, which are added in order.
 template <class OT, bool VEC>
@@ -445,6 +566,12 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const TableGrad a, i
   const int32_t id = keys[i1 - 1];
   if (id == a.V || keys[i1] != id) return;
   if (keys[i0] == id && i0 > 0 && keys[i0 - 1] == id) return;     // began earlier
+  // a run is longer than kShortRun just if more than that many of the kShortRun
+  // positions on either side of a boundary in it are its own
+  const int64_t near = i1 - kShortRun + threadIdx.x;
+  if (__syncthreads_count(threadIdx.x < 2 * kShortRun && near >= 0 && near < a.n &&
+                          keys[near] == id) <= kShortRun)
+    return;
   int64_t parts = 1;
   for (int64_t j = r + 1;; j += kJoinThreads) {
     const int64_t at = (j + threadIdx.x) * a.range;
@@ -510,7 +637,6 @@ int sum_threads(int d) {
 }  // namespace
 
 cudaError_t launch_lookup(Lookup a, int table_type, int out_type, int sm_count, cudaStream_t st) {
-  a.spans = (a.d + kLookSpan - 1) / kLookSpan;
   bool vec = on16(a.out, a.ld_out, type_size(out_type));
   if (table_type == TAB_E8M0)
     return launch_lookup_t<Mx4Row, MX4_E8M0>(a, out_type, vec, sm_count, st);
@@ -530,7 +656,7 @@ static int grad_range(int64_t n, int d, int sm_count) {
   const int64_t groups = (d + ct * 8 - 1) / (ct * 8), per = kSumThreads / ct;
   if (n > 65536) return (int)(32 * ((n + 65535) / 65536));
   int range = 32;
-  while (range > kSumBatch && (n + range - 1) / range * groups < 2 * sm_count * per) range /= 2;
+  while (range > 8 && (n + range - 1) / range * groups < 2 * sm_count * per) range /= 2;
   return range;
 }
 
@@ -569,16 +695,16 @@ cudaError_t launch_table_grad(TableGrad a, int src_type, int out_type, void* scr
   if (a.n == 0)                 // (not accumulating: the table's gradient is zero)
     return launch_pdl(fill_kernel<true>, dim3((unsigned)(2 * sm_count)), dim3(kFillThreads), 0, st,
                       a, type_size(out_type));
-  // a CTA for each tile of tokens, up to a portable cluster
-  int parts = 1;
-  while (parts < 8 && parts * kSortTile < a.n) parts *= 2;
-  int bits = 0;
+  // one CTA sorts a tile of tokens; longer lists take a portable cluster
+  const int parts = a.n <= kSortTile ? 1 : 8;
+  int bits = 1;
   while (((int64_t)1 << bits) <= a.V) ++bits;         // keys are 0 .. V
+  const int passes = (bits + kSortBits - 1) / kSortBits;
   cudaError_t e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)sizeof(SortSmem));
   if (e != cudaSuccess) return e;
   e = launch_pdl_cluster(sort_kernel, dim3(parts), dim3(kSortThreads), sizeof(SortSmem), st, parts,
-                         a, parts, (bits + kSortBits - 1) / kSortBits);
+                         a, parts, passes, (bits + passes - 1) / passes);
   if (e != cudaSuccess) return e;
   if (!a.add) {
     e = launch_pdl(fill_kernel<false>, dim3((unsigned)(2 * sm_count)), dim3(kFillThreads), 0, st, a,

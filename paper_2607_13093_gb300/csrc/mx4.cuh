@@ -43,7 +43,10 @@ __device__ __forceinline__ float exp2_int(int k) {      // 2^k for k in [-126, 1
 template <int FMT>
 __device__ __forceinline__ uint32_t mx4_scale(unsigned amax, int row_exp, float* step) {
   if constexpr (FMT == MX4_E4M3) {
-    const float v = __fdiv_rn(__uint_as_float(amax), 6.0f) * exp2_int(-row_exp);
+    // amax / 6 as IEEE division rounds it (as in mx4_codes below)
+    const float a = __uint_as_float(amax) * exp2_int(-row_exp), r6 = 1.0f / 6.0f;
+    float v = a * r6;
+    v = __fmaf_rn(__fmaf_rn(-6.0f, v, a), r6, v);
     const __nv_fp8_storage_t b = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
     const __half_raw h = __nv_cvt_fp8_to_halfraw(b, __NV_E4M3);
     *step = __half2float(__half(h)) * exp2_int(row_exp);
@@ -94,23 +97,27 @@ __device__ __forceinline__ uint32_t float_to_e2m1x8(const float (&t)[8]) {
   return c;
 }
 
-// Codes of eight values in units of `step` (0: a block that underflowed, all
-// codes zero).  x / step is rounded as IEEE division rounds it, from the
+// Codes of N values (8 to a word) in units of `step` (0: a block that underflowed,
+// all codes zero).  x / step is rounded as IEEE division rounds it, from the
 // correctly rounded reciprocal and two fused steps (Markstein, IBM J. Res.
 // Dev. 34, 1990): a division a value would cost as much as the pass's memory
 // traffic.  The rounded quotient meets a midpoint of two codes only where the
 // exact one does (step has 4 significant bits), so codes are the nearest ones
 // exactly.  An e8m0 step is a power of two and needs one product.
-template <int FMT>
-__device__ __forceinline__ uint32_t mx4_codes(const float (&x)[8], float step) {
+template <int FMT, int N>
+__device__ __forceinline__ void mx4_codes(const float (&x)[N], float step, uint32_t (&codes)[N / 8]) {
   const float r = step > 0.f ? __frcp_rn(step) : 0.f;
-  float t[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    t[j] = x[j] * r;
-    if constexpr (FMT == MX4_E4M3) t[j] = __fmaf_rn(__fmaf_rn(-t[j], step, x[j]), r, t[j]);
+  for (int w = 0; w < N / 8; ++w) {
+    float t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = x[8 * w + j];
+      t[j] = v * r;
+      if constexpr (FMT == MX4_E4M3) t[j] = __fmaf_rn(__fmaf_rn(-t[j], step, v), r, t[j]);
+    }
+    codes[w] = float_to_e2m1x8(t);
   }
-  return float_to_e2m1x8(t);
 }
 
 }  // namespace sph

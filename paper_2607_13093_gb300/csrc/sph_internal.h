@@ -369,7 +369,7 @@ struct Lookup {
   void* out;                // [n, d], row stride ld_out elements
   int64_t ld_out;
   unsigned* status;
-  int spans;                // set by the launch
+  int blocks, turns;        // set by the launch: blocks a token, spans of columns a block
 };
 cudaError_t launch_lookup(Lookup a, int table_type, int out_type, int sm_count, cudaStream_t st);
 

@@ -643,6 +643,11 @@ def _result(out, shape, dtype, dev, name):
 
 def sph_mx4_quantize(ctx, x, format=SPH_MX4_E4M3, *, out: Optional[Mx4] = None) -> Mx4:
     """Rows of x [R, d] (bf16, fp32 or fp16, any row stride) in 4 bits."""
+    if out is None:
+        r = _fast.mx4_quantize(_word(ctx), x, format)
+        if type(r) is tuple:
+            return Mx4(*r, x.shape[1], format)
+        _refused(ctx, r)
     typ, ld = _rows(x, "x")
     if out is None:
         out = mx4_empty(x.shape[0], x.shape[1], format, x.device)
@@ -655,6 +660,10 @@ def sph_mx4_quantize(ctx, x, format=SPH_MX4_E4M3, *, out: Optional[Mx4] = None) 
 
 def sph_mx4_dequantize(ctx, w: Mx4, *, out=None, dtype=torch.bfloat16):
     """The values that w stands for, [rows, d]."""
+    r = _fast.mx4_dequantize(_word(ctx), w, out, dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
     c = _mx4(w, w.codes.device)
     out = _result(out, (c.rows, w.d), dtype, w.codes.device, "out")
     typ, ld = _rows(out, "out", w.codes.device)
@@ -666,6 +675,10 @@ def sph_mx4_logits(ctx, h, W: Mx4, *, keep_ids=None, bias=None, planes=2, out=No
                    dtype=torch.float32):
     """Logits [R, n] of hidden states h [R, d] over the kept rows of a table in
     4 bits; h is held as `planes` terms of W's format.  fp32 or bf16."""
+    r = _fast.mx4_logits(_word(ctx), h, W, keep_ids, bias, planes, out, dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
     dev = h.device
     typ, ld = _rows(h, "h")
     c = _mx4(W, dev)
@@ -685,6 +698,10 @@ def sph_mx4_logits(ctx, h, W: Mx4, *, keep_ids=None, bias=None, planes=2, out=No
 def sph_embed(ctx, tokens, table, *, scale=1.0, padding_id=-1, out=None, dtype=None):
     """scale * table[tokens] as [T, d]: tokens int32 [T], table a tensor [V, d]
     (bf16, fp32 or fp16) or an Mx4.  dtype: the table's own, bf16 for an Mx4."""
+    r = _fast.embed(_word(ctx), tokens, table, scale, padding_id, out, dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
     dev = tokens.device
     _need(tokens, torch.int32, "tokens")
     _dense(dev, (tokens, "tokens", 0))
@@ -709,6 +726,10 @@ def sph_embed_grad(ctx, tokens, d_out, V: int, *, scale=1.0, padding_id=-1, accu
                    out=None, dtype=torch.float32):
     """The table's gradient [V, d] of sph_embed from d_out [T, d]; accumulate
     adds it to `out` (rows without a token are not touched)."""
+    r = _fast.embed_grad(_word(ctx), tokens, d_out, V, scale, padding_id, accumulate, out, dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
     dev = d_out.device
     _need(tokens, torch.int32, "tokens")
     _dense(dev, (tokens, "tokens", d_out.shape[0]))
