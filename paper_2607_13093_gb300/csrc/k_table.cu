@@ -72,35 +72,58 @@ constexpr int kLookSpan = kLookThreads * 8;    // columns of a block
 
 struct Mx4Row;     // tag of a table held in 4 bits (FMT says which)
 
+// A thread's eight columns of a table row as they lie in memory, and their values.
 template <class TT, int FMT, bool VEC>
-__device__ __forceinline__ void table_cols(const Lookup& a, int64_t id, int col, float (&v)[8]) {
-  if constexpr (FMT < 0) {
+struct Piece {           // dense rows
+  float v[8];
+  __device__ __forceinline__ void load(const Lookup& a, int64_t id, int col) {
     load_cols<TT, VEC>(static_cast<const TT*>(a.table) + id * a.ld_table, col, kLookThreads, a.d, v);
-  } else {
-    // (rows of codes and scales start on 16 bytes and end on a whole 32 columns)
-    const uint8_t* codes = static_cast<const uint8_t*>(a.table) + id * a.ld_table;
-    const uint8_t* scales = a.scales + id * a.ld_scales;
-    const float row = FMT == MX4_E4M3 ? a.row_scale[id] : 1.f;
-    if constexpr (VEC) {
-      if (col < a.d) {
-        e2m1x8_to_float(*reinterpret_cast<const uint32_t*>(codes + col / 2), v);
-        const float s = mx4_scale_value<FMT>(scales[col / Mx4<FMT>::kBlock]) * row;
+  }
+  __device__ __forceinline__ void values(float, float (&x)[8]) const {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= s;
-      }
-    } else {
+    for (int j = 0; j < 8; ++j) x[j] = v[j];
+  }
+};
+template <int FMT>
+struct Piece<Mx4Row, FMT, true> {      // eight consecutive columns in 4 bits
+  uint32_t codes;
+  uint8_t scale;
+  __device__ __forceinline__ void load(const Lookup& a, int64_t id, int col) {
+    codes = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.table) +
+                                               id * a.ld_table + col / 2);
+    scale = a.scales[id * a.ld_scales + col / Mx4<FMT>::kBlock];
+  }
+  __device__ __forceinline__ void values(float row, float (&x)[8]) const {
+    e2m1x8_to_float(codes, x);
+    const float s = mx4_scale_value<FMT>(scale) * row;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = col + j * kLookThreads;
-        if (c < a.d) {
-          float q[8];
-          e2m1x8_to_float((uint32_t)codes[c / 2] >> (c & 1) * 4 & 15u, q);
-          v[j] = q[0] * (mx4_scale_value<FMT>(scales[c / Mx4<FMT>::kBlock]) * row);
-        }
-      }
+    for (int j = 0; j < 8; ++j) x[j] *= s;
+  }
+};
+template <int FMT>
+struct Piece<Mx4Row, FMT, false> {     // columns kLookThreads apart
+  uint8_t codes[8], scale[8];
+  int odd;
+  __device__ __forceinline__ void load(const Lookup& a, int64_t id, int col) {
+    const uint8_t* c = static_cast<const uint8_t*>(a.table) + id * a.ld_table;
+    const uint8_t* s = a.scales + id * a.ld_scales;
+    odd = col & 1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int at = min(col + j * kLookThreads, a.d - 1);
+      codes[j] = c[at / 2];
+      scale[j] = s[at / Mx4<FMT>::kBlock];
     }
   }
-}
+  __device__ __forceinline__ void values(float row, float (&x)[8]) const {
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w |= (uint32_t)(codes[j] >> 4 * odd & 15) << 4 * j;
+    e2m1x8_to_float(w, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= mx4_scale_value<FMT>(scale[j]) * row;
+  }
+};
 
 // A block takes one token and `turns` spans of kLookSpan columns, U of them requested
 // together.
@@ -114,23 +137,28 @@ __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const Lookup a) {
   const int64_t id = a.tokens ? a.tokens[t] : t;
   const bool there = id >= 0 && id < a.V;
   if (!there && id != a.padding && first == 0) atomicOr(a.status, ERR_BAD_INDEX);
+  const float row = FMT == MX4_E4M3 && there ? a.row_scale[id] : 1.f;
   OT* out = static_cast<OT*>(a.out) + t * a.ld_out;
   for (int n = 0; n < a.turns; n += U) {
-    float v[U][8];
+    Piece<TT, FMT, VEC> piece[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
       const int col = first + (n + i) * kLookSpan;
-      if (there && n + i < a.turns && col < a.d) table_cols<TT, FMT, VEC>(a, id, col, v[i]);
+      if (there && n + i < a.turns && col < a.d) piece[i].load(a, id, col);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int col = first + (n + i) * kLookSpan;
       if (n + i >= a.turns || col >= a.d) break;
+      float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] *= a.scale;
-      store_cols<OT, VEC>(out, col, kLookThreads, a.d, v[i]);
+      for (int j = 0; j < 8; ++j) v[j] = 0.f;
+      if (there) {
+        piece[i].values(row, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= a.scale;
+      }
+      store_cols<OT, VEC>(out, col, kLookThreads, a.d, v);
     }
   }
 }
@@ -142,6 +170,9 @@ cudaError_t launch_lookup_v(Lookup a, int sm_count, cudaStream_t st) {
   a.turns = a.n >= (int64_t)sm_count * 16 ? spans : 1;
   a.blocks = (spans + a.turns - 1) / a.turns;
   const dim3 grid((unsigned)(a.n * a.blocks));
+  if (a.turns > 4 && FMT >= 0)          // (4-bit pieces are two registers each)
+    return launch_pdl(lookup_kernel<TT, FMT, OT, VEC, FMT >= 0 && VEC ? 8 : 4>, grid,
+                      dim3(kLookThreads), 0, st, a);
   if (a.turns > 1)
     return launch_pdl(lookup_kernel<TT, FMT, OT, VEC, 4>, grid, dim3(kLookThreads), 0, st, a);
   return launch_pdl(lookup_kernel<TT, FMT, OT, VEC, 1>, grid, dim3(kLookThreads), 0, st, a);
@@ -166,32 +197,39 @@ int type_size(int t) { return t == TAB_FP32 ? 4 : 2; }
 // ---------------------------------------------------------------------------
 // gradient: the sort
 // ---------------------------------------------------------------------------
-constexpr int kSortThreads = 512, kSortItems = 16, kSortTile = kSortThreads * kSortItems;
+constexpr int kSortThreads = 1024, kSortItems = 8, kSortTile = kSortThreads * kSortItems;
+constexpr int kSortShort = 2048;      // tokens that one CTA sorts
 constexpr int kSortBits = 9, kSortBins = 1 << kSortBits, kSortWarps = kSortThreads / 32;
 
 struct SortSmem {
   uint32_t hist[kSortBins];       // this CTA's count of each digit (read by the cluster)
   uint32_t base[kSortBins];       // where its next element of a digit goes
+  uint32_t local[kSortBins];      // the same within the current tile
+  uint32_t half[kSortBins];       // counts of the first half of the warps
   uint32_t part[kSortWarps];
   uint16_t warp[kSortWarps][kSortBins];
-  int32_t key[kSortTile];         // a sort of one tile stays here between passes
+  int32_t key[kSortTile];         // the tile in the order of its digits
   int32_t pos[kSortTile];
 };
 
 // One cluster sorts: stable radix passes over (id, position) with digits of at most
 // 9 bits, each CTA a contiguous part.  A warp's items are consecutive; equal
-// digits within a warp are ranked by match.any, its warps by a prefix over their
-// counts, the CTAs by one over theirs, read through distributed shared memory.
-// Up to kSortTile tokens (one CTA) the passes stay in shared memory; parts of one
-// tile get their counts from the ranking, longer ones from a pass of their own.
+// digits within a warp are ranked by votes, its warps by a prefix over their counts, the CTAs by one over theirs, read through distributed shared memory.
+// A tile is put in order in shared memory first and written from there, a digit's
+// elements side by side (one by one from the ranking, 8000 tokens took 24 us).  Up
+// to kSortTile tokens (one CTA) the passes stay in shared memory; parts of one tile
+// get their counts from the ranking, longer ones from a pass of their own.
 // Ids out of range become V, which sorts last.
+// FIRST: the call's first kernel.  Else it runs beside the one that zeroes rows, and
+// waits for that only at its end, so that the kernel after it may take both as done.
+template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, int parts, int passes,
                                                             int bits) {
   extern __shared__ __align__(16) uint8_t sort_raw[];
   SortSmem& s = *reinterpret_cast<SortSmem*>(sort_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)blockIdx.x;
-  ptx::griddep_wait();
+  if constexpr (FIRST) ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int part = (a.n + parts - 1) / parts;
   const int p0 = min(a.n, rank * part), p1 = min(a.n, p0 + part);
@@ -203,48 +241,61 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
     const int to = (passes - 1 - pass) & 1;
     const bool last = pass == passes - 1;
     auto key_of = [&](int i) {
-      if (pass > 0) return local ? s.key[i] : __ldcg(a.keys[to ^ 1] + i);
+      if (pass > 0) return __ldcg(a.keys[to ^ 1] + i);
       const int32_t id = a.tokens[i];
       return id >= 0 && id < a.V ? id : a.V;
     };
     auto digit = [&](int32_t k) { return (int)((uint32_t)k >> shift) & (bins - 1); };
-    // Where each digit's elements of this CTA start, from its own counts (thread b:
-    // digit b).
-    auto place = [&](uint32_t mine) {
-      uint32_t total = mine, below = 0;
-      if (parts > 1) {
-        s.hist[tid] = mine;
-        ptx::cluster_sync();
-        total = 0;
-        for (int c = 0; c < parts; ++c) {
-          uint32_t h;
-          asm volatile("ld.shared::cluster.u32 %0, [%1];"
-                       : "=r"(h)
-                       : "r"(ptx::mapa(ptx::smem_u32(&s.hist[tid]), (uint32_t)c))
-                       : "memory");
-          if (c < rank) below += h;
-          total += h;
-        }
-      }
-      uint32_t incl = total;
+    // exclusive sum over the block's threads (thread b: digit b)
+    auto sum_before = [&](uint32_t v) {
+      uint32_t incl = v;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
         if (lane >= o) incl += up;
       }
+      __syncthreads();             // (of s.part, read the last time)
       if (lane == 31) s.part[warp] = incl;
       __syncthreads();
-      uint32_t before = 0;
-      for (int w = 0; w < warp; ++w) before += s.part[w];
-      s.base[tid] = before + incl - total + below;
+      uint32_t w = lane < warp ? s.part[lane] : 0;
+      w = __reduce_add_sync(0xFFFFFFFFu, w);
+      return w + incl - v;
+    };
+    // where each digit's elements of this CTA start, from its own counts
+    auto place = [&](uint32_t mine) {
+      uint32_t total = mine, below = 0;
+      if (parts > 1) {
+        if (tid < kSortBins) s.hist[tid] = mine;
+        ptx::cluster_sync();
+        total = 0;
+        if (tid < kSortBins) {
+          uint32_t h[8];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            h[c] = 0;
+            if (c < parts)
+              asm volatile("ld.shared::cluster.u32 %0, [%1];"
+                           : "=r"(h[c])
+                           : "r"(ptx::mapa(ptx::smem_u32(&s.hist[tid]), (uint32_t)c))
+                           : "memory");
+          }
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            if (c < rank) below += h[c];
+            total += h[c];
+          }
+        }
+      }
+      const uint32_t at = sum_before(total) + below;
+      if (tid < kSortBins) s.base[tid] = at;
       __syncthreads();
     };
     if (!one) {
-      s.base[tid] = 0;
+      if (tid < kSortBins) s.base[tid] = 0;
       __syncthreads();
       for (int i = p0 + tid; i < p1; i += kSortThreads) atomicAdd(&s.base[digit(key_of(i))], 1u);
       __syncthreads();
-      const uint32_t mine = s.base[tid];
+      const uint32_t mine = tid < kSortBins ? s.base[tid] : 0;
       __syncthreads();
       place(mine);
     }
@@ -253,16 +304,30 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
       const int count = min(kSortTile, p1 - t0), rounds = (count + kSortThreads - 1) / kSortThreads;
       int32_t k[kSortItems], p[kSortItems];
       uint32_t r[kSortItems];
-      const int first = t0 + warp * 32 * rounds + lane;
+      const int first = t0 + warp * 32 * rounds + lane, stop = t0 + count;
+      // (no early end here: the loads of all rounds go out together)
 #pragma unroll
       for (int i = 0; i < kSortItems; ++i) {
-        if (i >= rounds) break;
         const int at = first + i * 32;
-        const bool in = at < t0 + count;
-        k[i] = in ? key_of(at) : 0;
-        p[i] = !in ? -1 : pass == 0 ? at : local ? s.pos[at] : __ldcg(a.pos[to ^ 1] + at);
-        if (pass == 0 && in && k[i] == a.V && a.tokens[at] != a.padding)
-          atomicOr(a.status, ERR_BAD_INDEX);
+        const bool in = i < rounds && at < stop;
+        if (pass == 0) {
+          k[i] = in ? a.tokens[at] : 0;
+          p[i] = in ? at : -1;
+        } else if (local) {
+          k[i] = in ? s.key[at] : 0;
+          p[i] = in ? s.pos[at] : -1;
+        } else {
+          k[i] = in ? __ldcg(a.keys[to ^ 1] + at) : 0;
+          p[i] = in ? __ldcg(a.pos[to ^ 1] + at) : -1;
+        }
+      }
+      if (pass == 0) {
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i) {
+          const bool out = k[i] < 0 || k[i] >= a.V;
+          if (out && k[i] != a.padding && p[i] >= 0) atomicOr(a.status, ERR_BAD_INDEX);
+          if (out) k[i] = a.V;
+        }
       }
       for (int b = lane; b < bins / 2; b += 32) reinterpret_cast<uint32_t*>(s.warp[warp])[b] = 0;
       __syncwarp();
@@ -270,9 +335,15 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
       for (int i = 0; i < kSortItems; ++i) {
         if (i >= rounds) break;
         const unsigned live = __ballot_sync(0xFFFFFFFFu, p[i] >= 0);
+        const int dg = digit(k[i]);
+        // lanes with this lane's digit, a vote a bit (match.any is several times slower)
+        unsigned same = live;
+#pragma unroll
+        for (int b = 0; b < kSortBits; ++b) {
+          const unsigned ones = __ballot_sync(0xFFFFFFFFu, dg >> b & 1);
+          same &= dg >> b & 1 ? ones : ~ones;
+        }
         if (p[i] >= 0) {
-          const int dg = digit(k[i]);
-          const unsigned same = __match_any_sync(live, dg);
           const uint32_t had = s.warp[warp][dg];
           r[i] = had + __popc(same & ((1u << lane) - 1));
           __syncwarp(live);
@@ -281,35 +352,56 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
         __syncwarp();
       }
       __syncthreads();
-      uint32_t run = 0;
-      if (tid < bins) {
+      // each warp's first place in a digit, and the digit's count (thread b < kSortBins:
+      // digit b), two threads a digit
+      const int dig = tid % kSortBins, w0 = tid / kSortBins * (kSortWarps / 2);
+      uint32_t c[kSortWarps / 2], run = 0;
 #pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) {
-          const uint32_t c = s.warp[w][tid];
-          s.warp[w][tid] = (uint16_t)run;
-          run += c;
+      for (int w = 0; w < kSortWarps / 2; ++w) {
+        c[w] = dig < bins ? s.warp[w0 + w][dig] : 0;
+        run += c[w];
+      }
+      if (w0 == 0) s.half[dig] = run;
+      __syncthreads();
+      uint32_t up = w0 ? s.half[dig] : 0;
+      const uint32_t mine = run;
+      if (dig < bins) {
+#pragma unroll
+        for (int w = 0; w < kSortWarps / 2; ++w) {
+          s.warp[w0 + w][dig] = (uint16_t)up;
+          up += c[w];
         }
       }
-      if (one) place(run);
-      else __syncthreads();
+      if (w0) s.hist[dig] = mine;
+      __syncthreads();
+      run = w0 ? 0 : run + s.hist[dig];
+      if (one && !local) place(run);
+      const uint32_t local_at = sum_before(run);
+      if (tid < kSortBins) s.local[tid] = local_at;
+      __syncthreads();
 #pragma unroll
       for (int i = 0; i < kSortItems; ++i) {
         if (i >= rounds) break;
         if (p[i] >= 0) {
           const int dg = digit(k[i]);
-          const uint32_t at = s.base[dg] + s.warp[warp][dg] + r[i];
-          if (local && !last) {
-            s.key[at] = k[i];
-            s.pos[at] = p[i];
-          } else {
-            a.keys[to][at] = k[i];
-            a.pos[to][at] = p[i];
-          }
+          const uint32_t at = s.local[dg] + s.warp[warp][dg] + r[i];
+          s.key[at] = k[i];
+          s.pos[at] = p[i];
         }
       }
       __syncthreads();
+      if (!local || last) {
+        for (int i = tid; i < count; i += kSortThreads) {
+          const int32_t key = s.key[i];
+          const int dg = digit(key);
+          const uint32_t at = local ? (uint32_t)i : s.base[dg] + (uint32_t)i - s.local[dg];
+          a.keys[to][at] = key;
+          a.pos[to][at] = s.pos[i];
+        }
+        __syncthreads();
+      }
       if (!one) {
-        s.base[tid] += run;
+        if (tid < kSortBins) s.base[tid] += run;
         __syncthreads();
       }
     }
@@ -317,12 +409,15 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
     // this one's counts when the next pass writes them
     if (parts > 1) ptx::cluster_sync();
   }
+  if (rank == 0 && tid == 0) a.pos[1][0] = 0;      // (free by now) the count of joins
+  if constexpr (!FIRST) ptx::griddep_wait();
 }
 
 // ---------------------------------------------------------------------------
 // gradient: zero rows
 // ---------------------------------------------------------------------------
 constexpr int kFillThreads = 512, kFillIds = 8192;
+constexpr int64_t kHeadBytes = 96 << 20;      // rows zeroed while the sort runs
 
 // Zeros, by one warp, over bytes of any alignment.
 __device__ __forceinline__ void zero_bytes(uint8_t* p, int64_t bytes, int lane) {
@@ -336,27 +431,40 @@ __device__ __forceinline__ void zero_bytes(uint8_t* p, int64_t bytes, int lane) 
   if (done + 2 * lane < bytes) *reinterpret_cast<uint16_t*>(p + done + 2 * lane) = 0;
 }
 
-// Block b zeroes the rows of its share of the ids that no token has: it marks
-// the ones that occur from the whole token list (a read of the L2, once per
-// kFillIds ids), so nothing is written twice.  Runs beside the sort, and waits
-// for it only at its end, so that the kernel after it may take both as done.
-// FIRST: it is the call's first kernel, and waits for the caller's work instead.
-template <bool FIRST>
-__global__ void __launch_bounds__(kFillThreads) fill_kernel(const TableGrad a, int elem) {
-  __shared__ uint32_t s_seen[kFillIds / 32];
+// Block `b` of `blocks` zeroes the rows of its share of the ids v_from .. v_to - 1 that
+// no token has: it marks the ones that occur from the whole token list (a read of
+// the L2, once per kFillIds ids), so nothing is written twice.
+__device__ __forceinline__ void zero_rows(const TableGrad& a, int64_t v_from, int64_t v_to, int b,
+                                          int blocks, int elem, uint32_t* s_seen) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t v0 = (int64_t)a.V * blockIdx.x / gridDim.x;
-  const int64_t v1 = (int64_t)a.V * (blockIdx.x + 1) / gridDim.x;
-  if constexpr (FIRST) ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
+  const int64_t v0 = v_from + (v_to - v_from) * b / blocks;
+  const int64_t v1 = v_from + (v_to - v_from) * (b + 1) / blocks;
+  auto mark = [&](int32_t token, int64_t base, int ids) {
+    const int64_t r = (int64_t)token - base;
+    if (r >= 0 && r < ids) atomicOr(&s_seen[r >> 5], 1u << (r & 31));
+  };
+  // (tokens on 16 bytes: four to a load, and four loads on their way)
+  const int quads = ((uintptr_t)a.tokens & 15) == 0 ? a.n / 4 : 0;
   for (int64_t base = v0; base < v1; base += kFillIds) {
     const int ids = (int)min((int64_t)kFillIds, v1 - base);
     for (int i = threadIdx.x; i < kFillIds / 32; i += kFillThreads) s_seen[i] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < a.n; i += kFillThreads) {
-      const int64_t r = (int64_t)a.tokens[i] - base;
-      if (r >= 0 && r < ids) atomicOr(&s_seen[r >> 5], 1u << (r & 31));
+    for (int i = threadIdx.x; i < quads; i += 4 * kFillThreads) {
+      int4 t[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        t[q] = i + q * kFillThreads < quads
+                   ? reinterpret_cast<const int4*>(a.tokens)[i + q * kFillThreads]
+                   : make_int4(-1, -1, -1, -1);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        mark(t[q].x, base, ids);
+        mark(t[q].y, base, ids);
+        mark(t[q].z, base, ids);
+        mark(t[q].w, base, ids);
+      }
     }
+    for (int i = 4 * quads + threadIdx.x; i < a.n; i += kFillThreads) mark(a.tokens[i], base, ids);
     __syncthreads();
     for (int r = warp; r < ids; r += kFillThreads / 32)
       if (!(s_seen[r >> 5] >> (r & 31) & 1))
@@ -364,7 +472,15 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const TableGrad a, i
                    (int64_t)a.d * elem, lane);
     __syncthreads();
   }
-  if constexpr (!FIRST) ptx::griddep_wait();
+}
+
+// The call's first kernel where it zeroes rows: the sort runs beside it, so it takes
+// about as many rows as the sort takes time, ids 0 .. v_to - 1.
+__global__ void __launch_bounds__(kFillThreads) head_kernel(const TableGrad a, int elem, int64_t v_to) {
+  __shared__ uint32_t s_seen[kFillIds / 32];
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  zero_rows(a, 0, v_to, (int)blockIdx.x, (int)gridDim.x, elem, s_seen);
 }
 
 // ---------------------------------------------------------------------------
@@ -372,7 +488,7 @@ __global__ void __launch_bounds__(kFillThreads) fill_kernel(const TableGrad a, i
 // ---------------------------------------------------------------------------
 constexpr int kSumThreads = 128;
 constexpr int kSumBytes = 256;      // shared memory of a thread: rows requested ahead
-constexpr int kShortRun = 32;       // positions of a run that one range takes whole
+constexpr int kShortRun = 16;       // (at most 32) positions of a run that one range takes whole
 
 // Columns of thread `u` of `ct` in column group g.
 template <bool VEC>
@@ -382,76 +498,87 @@ __device__ __forceinline__ int sum_col(int g, int u, int ct) {
 
 template <class OT, bool VEC>
 __device__ __forceinline__ void write_row(const TableGrad& a, int32_t id, int col, int ct,
-                                          const float (&sum)[8]) {
-  OT* row = static_cast<OT*>(a.out) + (int64_t)id * a.ld_out;
+                                          const float (&sum)[8], const float (&onto)[8]) {
   float v[8];
-  if (a.add) {
-    load_cols<OT, VEC>(row, col, ct, a.d, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += a.scale * sum[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = a.scale * sum[j];
-  }
-  store_cols<OT, VEC>(row, col, ct, a.d, v);
+  for (int j = 0; j < 8; ++j) v[j] = onto[j] + a.scale * sum[j];
+  store_cols<OT, VEC>(static_cast<OT*>(a.out) + (int64_t)id * a.ld_out, col, ct, a.d, v);
 }
 
-// The part of a run of equal ids around the boundary before position `at` (whose key
-// `id` is also that of at - 1): its start and end, exact for runs of at most
-// kShortRun positions; longer ones give more than kShortRun.
-__device__ __forceinline__ void run_around(const int32_t* keys, int n, int at, int32_t id, int* s,
-                                           int* e) {
-  int b = at - 1, f = at + 1;
-  while (b > 0 && at - b <= kShortRun && keys[b - 1] == id) --b;
-  while (f < n && f - b <= kShortRun && keys[f] == id) ++f;
-  *s = b;
-  *e = f;
-}
-
-// ct threads a range of a.range sorted positions and 8 ct columns (128 / ct
-// ranges a block).  A run of equal ids of at most kShortRun positions is summed by
+// ct threads (whole warps) a range of a.range sorted positions and 8 ct columns, 128 /
+// ct ranges a block.  A run of equal ids of at most kShortRun positions is summed by
 // the range that it begins in and written out; of a longer one each range sums its
 // own part, into slot 2 r of the partial sums where the run began earlier, into
-// slot 2 r + 1 where it begins in the range and goes on (written out where it
-// does neither).  A thread's columns of the next rows are on their way to its own
-// piece of shared memory while it adds: nothing is shared between threads.  (With
-// rows in registers the code for a run's end stood once for each of them:
-// 32768 rows x 4096 bf16 159 us.)
-template <class T, class OT, bool VEC>
+// slot 2 r + 1 where it begins in the range and goes on (written out where it does
+// neither).  Lanes hold the ids and positions of 32 sorted places each; a thread's
+// columns of the next rows are on their way to its own piece of shared memory
+// while it adds, and nothing is shared between threads.  ADD: so is what the table
+// holds for a run, requested with its first row (read at the run's end, it made each
+// run wait for memory: 8000 rows x 3584 41 us).  (With rows in registers the code for a
+// run's end stood once for each of them: 32768 rows x 4096 bf16 159 us.)
+template <class T, class OT, bool VEC, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int ct) {
-  __shared__ uint4 s_rows[kSumBytes / 16][kSumThreads];
+  // pieces of 16 bytes a slot: the row's, then the table's (not VEC: eight floats)
+  constexpr int kPieces = VEC ? (int)sizeof(T) / 2 : 2;
+  constexpr int kOnto = VEC && ADD ? (int)sizeof(OT) / 2 : 0;
+  constexpr int kFit = kSumBytes / 16 / (kPieces + kOnto);
+  constexpr int kAhead = !VEC ? 8 : kFit >= 16 ? 16 : kFit >= 8 ? 8 : 4;
+  __shared__ uint4 s_rows[kAhead * (kPieces + kOnto)][kSumThreads];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const int u = threadIdx.x % ct;
+  const int u = threadIdx.x % ct, lane = threadIdx.x & 31;
   const int group = (int)(blockIdx.x % a.groups);
   const int64_t r = (int64_t)(blockIdx.x / a.groups) * (kSumThreads / ct) + threadIdx.x / ct;
+  if (r * a.range >= a.n) return;
   const int col = sum_col<VEC>(group, u, ct);
-  if (r * a.range >= a.n || col >= a.d) return;
+  const bool active = col < a.d;
   const int i0 = (int)(r * a.range), i1 = min(a.n, i0 + a.range);
   const int32_t* keys = a.keys[0];
   const int32_t* pos = a.pos[0];
+  auto window = [&](const int32_t* list, int from) {       // 32 places from `from`, -1 outside
+    const int at = from + lane;
+    return at >= 0 && at < a.n ? list[at] : -1;
+  };
+  auto matches = [&](int32_t w, int32_t id) { return __popc(__ballot_sync(0xFFFFFFFFu, w == id)); };
+  const int32_t before = window(keys, i0 - 32), first = window(keys, i0);
+  const int32_t tail = window(keys, i1 - 32), after = window(keys, i1);
   int begin = i0, end = i1;
   bool open_left = false, open_right = false;
-  if (i0 > 0 && keys[i0 - 1] == keys[i0]) {
-    int s, e;
-    run_around(keys, a.n, i0, keys[i0], &s, &e);
-    if (e - s > kShortRun) open_left = true;
-    else begin = e;
+  const int32_t id0 = __shfl_sync(0xFFFFFFFFu, first, 0);
+  const int32_t id1 = __shfl_sync(0xFFFFFFFFu, tail, 31);
+  // (a run's places are neighbours, so its length around a boundary is the count of
+  // its id on both sides, exact up to 32)
+  if (__shfl_sync(0xFFFFFFFFu, before, 31) == id0) {
+    const int f = matches(first, id0);
+    if (matches(before, id0) + f > kShortRun) open_left = true;
+    else begin = i0 + f;
   }
   if (begin >= i1) return;
-  if (i1 < a.n && keys[i1 - 1] == keys[i1]) {
-    int s, e;
-    run_around(keys, a.n, i1, keys[i1], &s, &e);
-    if (e - s > kShortRun) open_right = true;
-    else end = e;
+  if (__shfl_sync(0xFFFFFFFFu, after, 0) == id1) {
+    const int f = matches(after, id1);
+    if (matches(tail, id1) + f > kShortRun) open_right = true;
+    else end = i1 + f;
   }
-  float acc[8];
+  if (id1 == a.V) {        // tokens without a row sort last: none of them, from the first on
+    int lo = begin;
+    while (lo < end) {
+      const int mid = (lo + end) / 2;
+      if (keys[mid] == a.V) end = mid;
+      else lo = mid + 1;
+    }
+    open_right = false;
+    if (end == begin) return;
+  }
+  float acc[8], onto[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-  int32_t cur = keys[begin];
+  for (int j = 0; j < 8; ++j) acc[j] = onto[j] = 0.f;
+  int32_t key = window(keys, begin), at = window(pos, begin);
+  int32_t next_key = window(keys, begin + 32), next_at = window(pos, begin + 32);
+  int32_t cur = __shfl_sync(0xFFFFFFFFu, key, 0);
   auto flush = [&](bool right) {
+    if (!active) return;
     if (!open_left && !right) {
-      write_row<OT, VEC>(a, cur, col, ct, acc);
+      write_row<OT, VEC>(a, cur, col, ct, acc, onto);
     } else {
       float* p = a.partial + (2 * r + (open_left ? 0 : 1)) * a.ld_partial + group * ct * 8 + u * 8;
       reinterpret_cast<float4*>(p)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -469,167 +596,208 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] += x[j];
   };
-  // (ids without a row of their own sort last)
-  while (end > begin && keys[end - 1] == a.V) {
-    // a whole range of them, or its tail: they end the list, so halve towards the first
-    int lo = begin, hi = end - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (keys[mid] == a.V) hi = mid;
-      else lo = mid + 1;
-    }
-    end = lo;
-    open_right = false;
-  }
-  if (end == begin) return;
-  auto row_of = [&](int i) { return static_cast<const T*>(a.d_out) + (int64_t)pos[i] * a.ld_d_out; };
-  if constexpr (VEC) {
-    constexpr int kPieces = (int)sizeof(T) / 2, kAhead = kSumBytes / 16 / kPieces;
-    auto request = [&](int i) {
-      if (i < end) {
-        const T* row = row_of(i) + col;
-        const int slot = (i - begin) % kAhead * kPieces;
+  // row of the place `q` after the window's first (less than 64)
+  auto row_of = [&](int q) {
+    const int32_t t = __shfl_sync(0xFFFFFFFFu, q < 32 ? at : next_at, q & 31);
+    return static_cast<const T*>(a.d_out) + (int64_t)t * a.ld_d_out;
+  };
+  auto copy16 = [&](uint4* dst, const void* row, int q, int size) {
+    // columns past the row's last are zeros, and not read
+    const int bytes = min(16, max(0, (a.d - col) * size - 16 * q));
+    if (active)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)),
+                   "l"(static_cast<const uint4*>(row) + (bytes > 0 ? q : 0)), "r"(bytes)
+                   : "memory");
+  };
+  int32_t asked = -1;                       // the id of the last place requested
+  auto request = [&](int w0, int i) {       // (VEC) place i, of the window from w0
+    if (i < end) {
+      const int slot = (i - begin) % kAhead * (kPieces + kOnto);
+      const T* row = row_of(i - w0) + col;
 #pragma unroll
-        for (int q = 0; q < kPieces; ++q) {
-          // columns past the row's last are zeros, and not read
-          const int bytes = min(16, max(0, (a.d - col) * (int)sizeof(T) - 16 * q));
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                           ptx::smem_u32(&s_rows[slot + q][threadIdx.x])),
-                       "l"(bytes > 0 ? reinterpret_cast<const uint4*>(row) + q
-                                     : reinterpret_cast<const uint4*>(row)),
-                       "r"(bytes)
-                       : "memory");
+      for (int q = 0; q < kPieces; ++q) copy16(&s_rows[slot + q][threadIdx.x], row, q, sizeof(T));
+      if constexpr (ADD) {
+        const int32_t k = __shfl_sync(0xFFFFFFFFu, i - w0 < 32 ? key : next_key, (i - w0) & 31);
+        if (k != asked) {
+          const OT* t = static_cast<const OT*>(a.out) + (int64_t)k * a.ld_out + col;
+#pragma unroll
+          for (int q = 0; q < kOnto; ++q)
+            copy16(&s_rows[slot + kPieces + q][threadIdx.x], t, q, sizeof(OT));
+          asked = k;
         }
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-#pragma unroll
-    for (int i = 0; i < kAhead - 1; ++i) request(begin + i);
-    for (int i = begin; i < end; ++i) {
-      request(i + kAhead - 1);
-      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-      uint4 w[kPieces];
-#pragma unroll
-      for (int q = 0; q < kPieces; ++q)
-        w[q] = s_rows[(i - begin) % kAhead * kPieces + q][threadIdx.x];
-      const T* e = reinterpret_cast<const T*>(w);
-      float x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = to_f32(e[j]);
-      add(keys[i], x);
     }
-  } else {
-    constexpr int kAhead = kSumBytes / 32;
-    for (int b = begin; b < end; b += kAhead) {
-      const int m = min(kAhead, end - b);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if constexpr (VEC) {
+    for (int i = 0; i < kAhead - 1; ++i) request(begin, begin + i);
+  }
+  int32_t last = -1;
+  for (int w0 = begin; w0 < end; w0 += 32) {
+    const int count = min(32, end - w0);
+    if constexpr (VEC) {
+      for (int q = 0; q < count; ++q) {
+        request(w0, w0 + q + kAhead - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+        uint4 w[kPieces];
+        const int slot = (w0 + q - begin) % kAhead * (kPieces + kOnto);
 #pragma unroll
-      for (int h = 0; h < kAhead; h += 4) {
-        float x[4][8];
+        for (int h = 0; h < kPieces; ++h) w[h] = s_rows[slot + h][threadIdx.x];
+        const T* e = reinterpret_cast<const T*>(w);
+        float x[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (h + q < m) load_cols<T, false>(row_of(b + h + q), col, ct, a.d, x[q]);
+        for (int j = 0; j < 8; ++j) x[j] = to_f32(e[j]);
+        const int32_t k = __shfl_sync(0xFFFFFFFFu, key, q);
+        add(k, x);
+        if constexpr (ADD) {
+          if (w0 + q == begin || k != last) {      // (a run's first row: what it is added to)
+            uint4 t[kOnto];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (h + q < m) {
-            s_rows[2 * (h + q)][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][0]);
-            s_rows[2 * (h + q) + 1][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][4]);
+            for (int h = 0; h < kOnto; ++h) t[h] = s_rows[slot + kPieces + h][threadIdx.x];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) onto[j] = to_f32(reinterpret_cast<const OT*>(t)[j]);
           }
+          last = k;
+        }
       }
-      for (int q = 0; q < m; ++q) {
-        const uint4 lo = s_rows[2 * q][threadIdx.x], hi = s_rows[2 * q + 1][threadIdx.x];
-        const float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z),
-                            __uint_as_float(lo.w), __uint_as_float(hi.x), __uint_as_float(hi.y),
-                            __uint_as_float(hi.z), __uint_as_float(hi.w)};
-        add(keys[b + q], x);
+    } else {
+      for (int b = 0; b < count; b += kAhead) {
+        const int m = min(kAhead, count - b);
+        for (int h = 0; h < m; h += 4) {
+          float x[4][8];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const T* row = row_of(min(b + h + q, 31));
+            if (h + q < m) load_cols<T, false>(row, col, ct, a.d, x[q]);
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (h + q < m) {
+              s_rows[2 * (h + q)][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][0]);
+              s_rows[2 * (h + q) + 1][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][4]);
+            }
+        }
+        for (int q = 0; q < m; ++q) {
+          const uint4 lo = s_rows[2 * q][threadIdx.x], hi = s_rows[2 * q + 1][threadIdx.x];
+          const float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z),
+                              __uint_as_float(lo.w), __uint_as_float(hi.x), __uint_as_float(hi.y),
+                              __uint_as_float(hi.z), __uint_as_float(hi.w)};
+          const int32_t k = __shfl_sync(0xFFFFFFFFu, key, b + q);
+          add(k, x);
+          if (ADD && k != last && active)
+            load_cols<OT, false>(static_cast<const OT*>(a.out) + (int64_t)k * a.ld_out, col, ct, a.d,
+                                 onto);
+          last = k;
+        }
       }
     }
+    key = next_key;
+    at = next_at;
+    next_key = window(keys, w0 + 64);
+    next_at = window(pos, w0 + 64);
   }
   flush(open_right);
+  if (open_right && !open_left && group == 0 && u == 0)        // a run to join starts here
+    a.keys[1][atomicAdd(&a.pos[1][0], 1)] = (int32_t)r;
 }
 
-constexpr int kJoinThreads = 256;
-
-// A block for each range and column group; it goes on only where a run of more than
-// kShortRun positions begins in the range and crosses its end.  The run's parts (slot 2 r + 1, then slot 2 j of
-// the ranges j it reaches) are shared by the block's thread groups in contiguous
-// shares, which are added in order.
+// The last kernel.  Its first `joins` blocks add up the runs that cross ranges, from
+// the list that the sums left (in any order: each is summed by itself); the others
+// zero the rows of ids v_from .. V - 1 meanwhile.  A run's parts (slot 2 r + 1 of the
+// range r it begins in, then slot 2 j of the ranges j it reaches) are shared by the
+// block's thread groups in contiguous shares, which are added in order.
 template <class OT, bool VEC>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const TableGrad a, int ct) {
+__global__ void __launch_bounds__(kFillThreads) tail_kernel(const TableGrad a, int ct, int joins,
+                                                            int64_t v_from) {
+  constexpr int kJoinThreads = kFillThreads;
   __shared__ float s_sum[kJoinThreads * 8];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const int group = (int)(blockIdx.x % a.groups);
-  const int64_t r = blockIdx.x / a.groups;
-  const int64_t i0 = r * a.range, i1 = i0 + a.range;
-  const int32_t* keys = a.keys[0];
-  if (i1 >= a.n) return;
-  const int32_t id = keys[i1 - 1];
-  if (id == a.V || keys[i1] != id) return;
-  if (keys[i0] == id && i0 > 0 && keys[i0 - 1] == id) return;     // began earlier
-  // a run is longer than kShortRun just if more than that many of the kShortRun
-  // positions on either side of a boundary in it are its own
-  const int64_t near = i1 - kShortRun + threadIdx.x;
-  if (__syncthreads_count(threadIdx.x < 2 * kShortRun && near >= 0 && near < a.n &&
-                          keys[near] == id) <= kShortRun)
+  if ((int)blockIdx.x >= joins) {
+    zero_rows(a, v_from, a.V, (int)blockIdx.x - joins, (int)gridDim.x - joins, (int)sizeof(OT),
+              reinterpret_cast<uint32_t*>(s_sum));
     return;
-  int64_t parts = 1;
-  for (int64_t j = r + 1;; j += kJoinThreads) {
-    const int64_t at = (j + threadIdx.x) * a.range;
-    const int c = __syncthreads_count(at < a.n && keys[at] == id);
-    parts += c;
-    if (c < kJoinThreads) break;
   }
-  const int u = threadIdx.x % ct, share = threadIdx.x / ct, shares = kJoinThreads / ct;
-  const int col = sum_col<VEC>(group, u, ct);
-  float sum[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-  if (col < a.d) {
-    const int64_t q1 = parts * (share + 1) / shares;
-#pragma unroll 4
-    for (int64_t q = parts * share / shares; q < q1; ++q) {
-      const float4* p = reinterpret_cast<const float4*>(
-          a.partial + (q == 0 ? 2 * r + 1 : 2 * (r + q)) * a.ld_partial + group * ct * 8 + u * 8);
-      const float4 x = p[0], y = p[1];
-      sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-      sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+  const int32_t* keys = a.keys[0];
+  const int64_t work = (int64_t)a.pos[1][0] * a.groups;
+  for (int64_t item = blockIdx.x; item < work; item += joins) {
+    const int group = (int)(item % a.groups);
+    const int64_t r = a.keys[1][item / a.groups];
+    const int32_t id = keys[(r + 1) * a.range];
+    int64_t parts = 1;
+    for (int64_t j = r + 1;; j += kJoinThreads) {
+      const int64_t at = (j + threadIdx.x) * a.range;
+      const int c = __syncthreads_count(at < a.n && keys[at] == id);
+      parts += c;
+      if (c < kJoinThreads) break;
     }
+    const int u = threadIdx.x % ct, share = threadIdx.x / ct, shares = kJoinThreads / ct;
+    const int col = sum_col<VEC>(group, u, ct);
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+    if (col < a.d) {
+      const int64_t q1 = parts * (share + 1) / shares;
+#pragma unroll 8
+      for (int64_t q = parts * share / shares; q < q1; ++q) {
+        const float4* p = reinterpret_cast<const float4*>(
+            a.partial + (q == 0 ? 2 * r + 1 : 2 * (r + q)) * a.ld_partial + group * ct * 8 + u * 8);
+        const float4 x = p[0], y = p[1];
+        sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+        sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s_sum[j * kJoinThreads + threadIdx.x] = sum[j];
+    __syncthreads();
+    if (share == 0 && col < a.d) {
+      for (int h = 1; h < shares; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += s_sum[j * kJoinThreads + h * ct + u];
+      float onto[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) onto[j] = 0.f;
+      if (a.add)
+        load_cols<OT, VEC>(static_cast<const OT*>(a.out) + (int64_t)id * a.ld_out, col, ct, a.d, onto);
+      write_row<OT, VEC>(a, id, col, ct, sum, onto);
+    }
+    __syncthreads();
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) s_sum[j * kJoinThreads + threadIdx.x] = sum[j];
-  __syncthreads();
-  if (share > 0 || col >= a.d) return;
-  for (int h = 1; h < shares; ++h)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] += s_sum[j * kJoinThreads + h * ct + u];
-  write_row<OT, VEC>(a, id, col, ct, sum);
 }
 
 template <class T, class OT, bool VEC>
-cudaError_t launch_sums(const TableGrad& a, int ct, cudaStream_t st) {
+cudaError_t launch_sums(const TableGrad& a, int ct, int64_t v_from, int sm_count, cudaStream_t st) {
   const int64_t ranges = (a.n + (int64_t)a.range - 1) / a.range;
   const int per = kSumThreads / ct;
-  cudaError_t e = launch_pdl(sum_kernel<T, OT, VEC>,
+  cudaError_t e = launch_pdl(a.add ? sum_kernel<T, OT, VEC, true> : sum_kernel<T, OT, VEC, false>,
                              dim3((unsigned)((ranges + per - 1) / per * a.groups)),
                              dim3(kSumThreads), 0, st, a, ct);
-  if (e != cudaSuccess || ranges < 2) return e;
-  return launch_pdl(join_kernel<OT, VEC>, dim3((unsigned)((ranges - 1) * a.groups)),
-                    dim3(kJoinThreads), 0, st, a, ct);
+  if (e != cudaSuccess) return e;
+  const int64_t most = (ranges - 1) * a.groups, grid = 2 * (int64_t)sm_count;
+  const int joins = a.n <= kShortRun ? 0 : (int)(most < grid ? most : grid);
+  const int zeros = v_from < a.V ? 2 * sm_count : 0;
+  if (joins + zeros == 0) return e;
+  return launch_pdl(tail_kernel<OT, VEC>, dim3((unsigned)(joins + zeros)), dim3(kFillThreads), 0, st,
+                    a, ct, joins, v_from);
 }
 template <class T, class OT>
-cudaError_t launch_sums_v(const TableGrad& a, int ct, bool vec, cudaStream_t st) {
-  return vec ? launch_sums<T, OT, true>(a, ct, st) : launch_sums<T, OT, false>(a, ct, st);
+cudaError_t launch_sums_v(const TableGrad& a, int ct, bool vec, int64_t v_from, int sm_count,
+                          cudaStream_t st) {
+  return vec ? launch_sums<T, OT, true>(a, ct, v_from, sm_count, st)
+             : launch_sums<T, OT, false>(a, ct, v_from, sm_count, st);
 }
 template <class T>
-cudaError_t launch_sums_o(const TableGrad& a, int ct, int out_type, bool vec, cudaStream_t st) {
-  if (out_type == TAB_FP32) return launch_sums_v<T, float>(a, ct, vec, st);
-  if (out_type == TAB_BF16) return launch_sums_v<T, __nv_bfloat16>(a, ct, vec, st);
-  return launch_sums_v<T, __half>(a, ct, vec, st);
+cudaError_t launch_sums_o(const TableGrad& a, int ct, int out_type, bool vec, int64_t v_from,
+                          int sm_count, cudaStream_t st) {
+  if (out_type == TAB_FP32) return launch_sums_v<T, float>(a, ct, vec, v_from, sm_count, st);
+  if (out_type == TAB_BF16) return launch_sums_v<T, __nv_bfloat16>(a, ct, vec, v_from, sm_count, st);
+  return launch_sums_v<T, __half>(a, ct, vec, v_from, sm_count, st);
 }
 
-// Threads that share a range's columns: enough for the row, at most 128.
+// Threads that share a range's columns: enough for the row, a warp at least, at most
+// 128.
 int sum_threads(int d) {
-  int ct = 4;
+  int ct = 32;
   while (ct < kSumThreads && ct * 8 < d) ct *= 2;
   return ct;
 }
@@ -650,13 +818,13 @@ cudaError_t launch_lookup(Lookup a, int table_type, int out_type, int sm_count, 
 }
 
 // Sorted positions a range holds: 32, fewer where that would leave the SMs without
-// two blocks each, more where a run through all ranges would make too many parts.
+// sixteen blocks each, more where a run through all ranges would make too many parts.
 static int grad_range(int64_t n, int d, int sm_count) {
   const int ct = sum_threads(d);
   const int64_t groups = (d + ct * 8 - 1) / (ct * 8), per = kSumThreads / ct;
   if (n > 65536) return (int)(32 * ((n + 65535) / 65536));
   int range = 32;
-  while (range > 8 && (n + range - 1) / range * groups < 2 * sm_count * per) range /= 2;
+  while (range > 8 && (n + range - 1) / range * groups < 16 * sm_count * per) range /= 2;
   return range;
 }
 
@@ -668,11 +836,11 @@ size_t grad_scratch_bytes(int64_t n, int d, int sm_count) {
 }
 
 // At least what any call of up to n tokens and d columns takes: in ranges of fewer
-// than 32 positions a call has at most 4 sm_count * 128 thread columns of partial
+// than 32 positions a call has at most 32 sm_count * 128 thread columns of partial
 // sums, else at most 2048 ranges.
 size_t grad_reserve_bytes(int64_t n, int64_t d, int sm_count) {
   const size_t list = ((size_t)n * 4 + 255) / 256 * 256;
-  const size_t few = (size_t)sm_count * 4 * kSumThreads * 64;
+  const size_t few = (size_t)sm_count * 32 * kSumThreads * 64;
   const int64_t ranges = n / 32 + 1 < 2048 ? n / 32 + 1 : 2048;
   const size_t many = (size_t)ranges * 2 * ((d + 1023) / 1024 * 1024) * 4;
   return 4 * list + (few > many ? few : many);
@@ -692,30 +860,33 @@ cudaError_t launch_table_grad(TableGrad a, int src_type, int out_type, void* scr
     at += 2 * list;
   }
   a.partial = reinterpret_cast<float*>(at);
-  if (a.n == 0)                 // (not accumulating: the table's gradient is zero)
-    return launch_pdl(fill_kernel<true>, dim3((unsigned)(2 * sm_count)), dim3(kFillThreads), 0, st,
-                      a, type_size(out_type));
-  // one CTA sorts a tile of tokens; longer lists take a portable cluster
-  const int parts = a.n <= kSortTile ? 1 : 8;
+  cudaError_t e = cudaSuccess;
+  int64_t head = 0;             // ids whose rows are zeroed beside the sort
+  if (!a.add) {
+    const int64_t row = (int64_t)a.d * type_size(out_type);
+    head = a.n == 0 ? a.V : kHeadBytes / row;
+    if (head > a.V) head = a.V;
+    e = launch_pdl(head_kernel, dim3((unsigned)(2 * sm_count)), dim3(kFillThreads), 0, st, a,
+                   type_size(out_type), head);
+    if (e != cudaSuccess || a.n == 0) return e;
+  }
+  // one CTA sorts a short list; longer ones take a portable cluster
+  const int parts = a.n <= kSortShort ? 1 : 8;
   int bits = 1;
   while (((int64_t)1 << bits) <= a.V) ++bits;         // keys are 0 .. V
   const int passes = (bits + kSortBits - 1) / kSortBits;
-  cudaError_t e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)sizeof(SortSmem));
+  auto sort = a.add ? sort_kernel<true> : sort_kernel<false>;
+  e = cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortSmem));
   if (e != cudaSuccess) return e;
-  e = launch_pdl_cluster(sort_kernel, dim3(parts), dim3(kSortThreads), sizeof(SortSmem), st, parts,
-                         a, parts, passes, (bits + passes - 1) / passes);
+  e = launch_pdl_cluster(sort, dim3(parts), dim3(kSortThreads), sizeof(SortSmem), st, parts, a, parts,
+                         passes, (bits + passes - 1) / passes);
   if (e != cudaSuccess) return e;
-  if (!a.add) {
-    e = launch_pdl(fill_kernel<false>, dim3((unsigned)(2 * sm_count)), dim3(kFillThreads), 0, st, a,
-                   type_size(out_type));
-    if (e != cudaSuccess) return e;
-  }
+  const int64_t v_from = a.add ? a.V : head;
   const bool vec = on16(a.out, a.ld_out, type_size(out_type)) &&
                    on16(a.d_out, a.ld_d_out, type_size(src_type));
-  if (src_type == TAB_FP32) return launch_sums_o<float>(a, ct, out_type, vec, st);
-  if (src_type == TAB_BF16) return launch_sums_o<__nv_bfloat16>(a, ct, out_type, vec, st);
-  return launch_sums_o<__half>(a, ct, out_type, vec, st);
+  if (src_type == TAB_FP32) return launch_sums_o<float>(a, ct, out_type, vec, v_from, sm_count, st);
+  if (src_type == TAB_BF16) return launch_sums_o<__nv_bfloat16>(a, ct, out_type, vec, v_from, sm_count, st);
+  return launch_sums_o<__half>(a, ct, out_type, vec, v_from, sm_count, st);
 }
 
 }  // namespace sph
