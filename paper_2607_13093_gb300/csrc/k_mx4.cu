@@ -123,6 +123,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) quant_kernel(const Mx4Q
   __shared__ T s_stage[kThreads / 32][32 * (kCols + 2)];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
+  if constexpr (OPERAND) {
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.zeros;
+         i += (int64_t)gridDim.x * kThreads)
+      a.zero[i] = 0;
+  }
   const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (row >= a.rows) return;                           // (whole warps; TPR >= 128: whole blocks)
@@ -167,7 +172,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) quant_kernel(const Mx4Q
     const int tile = (int)(row / a.tile_rows), r = (int)(row % a.tile_rows);
     words = a.tile_words;
     at_scale = (int64_t)tile * a.tile_bytes + r * words * 4;
-    step = a.tile_rows * words * 4;
+    step = a.stage_bytes;
   } else {
     words = 1;
     at_scale = row * a.ld_scales;

@@ -759,7 +759,7 @@ sph_status sph_reserve(sph_ctx* ctx, int64_t max_rows, int64_t max_n_keep,
   const size_t v = verify_reserve_bytes(max_rows, max_n_keep);
   if (v > need) need = v;
   // the operators on a vocabulary table
-  const size_t m = sph::mx4_gemm_reserve_bytes(max_rows, max_d);
+  const size_t m = sph::mx4_gemm_reserve_bytes(max_rows, max_n_keep, max_d, ctx->sm_count);
   if (m > need) need = m;
   const size_t t = sph::grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
   if (t > need) need = t;
@@ -1393,7 +1393,9 @@ sph_status sph_mx4_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type, int6
   st = host_check_ids(ctx, keep_ids, n_keep, W->rows);
   if (st) return st;
   const int fmt = mx4_format(W);
-  st = ensure_scratch(ctx, sph::mx4_gemm_scratch_bytes(rows, n_keep, (int)W->d, planes, fmt));
+  const sph::Mx4Plan plan{rows, n_keep, (int)W->d, planes, fmt, ctx->sm_count, ctx->pair_units,
+                          pair_mode(ctx), ctx->tc_schedule};
+  st = ensure_scratch(ctx, sph::mx4_gemm_scratch_bytes(plan));
   if (st) return st;
   sph::Mx4Gemm m{};
   m.x = h; m.ld_x = ld_h; m.rows = (int)rows; m.d = (int)W->d; m.x_type = h_type;
@@ -1403,8 +1405,8 @@ sph_status sph_mx4_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type, int6
   m.w_row = W->row_scale; m.V = W->rows; m.bias = bias; m.ids = keep_ids; m.n = (int)n_keep;
   m.out = out; m.ld_out = ld_out; m.out_type = out_type; m.status = ctx->status;
   return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
-                         return sph::launch_mx4_gemm(m, ctx->scratch, ctx->spin_limit,
-                                                     ctx->sm_count, ctx->stream);
+                         return sph::launch_mx4_gemm(m, plan, ctx->scratch, ctx->spin_limit,
+                                                     ctx->stream);
                        }), "4-bit product launch");
 }
 

@@ -322,9 +322,11 @@ struct Mx4Quant {
   int planes;               // terms; 1 in the table form
   // operand form
   int64_t plane_codes, plane_scales;    // bytes between terms
-  int tile_rows;            // rows of a tile; its scales are [stage][tile_rows][tile_words]
-  int tile_words;           // 4-byte words, tile_bytes in all
-  int64_t tile_bytes;
+  int tile_rows;            // rows of a tile; its scales are [stage][term][tile_rows]
+  int tile_words;           // [tile_words] 4-byte words
+  int64_t stage_bytes, tile_bytes;
+  unsigned* zero;           // words to clear
+  int zeros;
   int aligned;              // set by the launch: rows start on 16 bytes
 };
 cudaError_t launch_mx4_quant(Mx4Quant a, int fmt, int x_type, bool operand, cudaStream_t st);
@@ -348,9 +350,17 @@ struct Mx4Gemm {
   int out_type;             // TAB_FP32 or TAB_BF16
   unsigned* status;
 };
-size_t mx4_gemm_scratch_bytes(int64_t rows, int64_t n, int d, int planes, int fmt);
-size_t mx4_gemm_reserve_bytes(int64_t rows, int64_t d);
-cudaError_t launch_mx4_gemm(const Mx4Gemm& g, void* scratch, long long spin_limit, int sm_count,
+// What its work split depends on.
+struct Mx4Plan {
+  int64_t rows, n;
+  int d, planes, fmt;
+  int sm_count, pair_units;     // SMs, CTA pairs that fit at once
+  int pair_mode;                // 0 never, 1 where it pays, 2 always
+  int schedule;                 // 0 automatic, 1 whole tiles, 2 ranges of stages
+};
+size_t mx4_gemm_scratch_bytes(const Mx4Plan& a);
+size_t mx4_gemm_reserve_bytes(int64_t rows, int64_t n, int64_t d, int sm_count);
+cudaError_t launch_mx4_gemm(const Mx4Gemm& g, const Mx4Plan& a, void* scratch, long long spin_limit,
                             cudaStream_t st);
 
 // Lookup of table rows (k_table.cu).

@@ -204,6 +204,41 @@ def test_product_of_kept_rows(sph, ctx, fmt, rows, kind, out):
     assert_close(f64(y), want, bound, kind)
 
 
+@pytest.fixture
+def split(request, sph, ctx):
+    """The context with CTA pairs and the schedule as asked for."""
+    pair, schedule = request.param
+    ctx.set_option(sph.SPH_OPT_TC_PAIR, pair)
+    ctx.set_option(sph.SPH_OPT_TC_SCHEDULE, schedule)
+    yield request.param
+    ctx.set_option(sph.SPH_OPT_TC_PAIR, 0)
+    ctx.set_option(sph.SPH_OPT_TC_SCHEDULE, 0)
+
+
+@pytest.mark.parametrize("split", [(1, 1), (1, 2), (2, 1), (2, 2)], indirect=True)
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("planes", [1, 2, 4])
+@pytest.mark.parametrize("rows,V,d,keep", [(1, 100, 300, False), (33, 3000, 1300, True),
+                                           (70, 129, 4000, False), (240, 900, 700, True),
+                                           (500, 257, 256, False)])
+def test_product_on_pairs_and_in_ranges(sph, ctx, split, fmt, planes, rows, V, d, keep):
+    rng = np.random.default_rng(rows)
+    w, table = held(sph, ctx, V, d, fmt, V + d)
+    h = make_x(rows, d, torch.bfloat16, rows)
+    ids = None
+    if keep:
+        ids = np.sort(np.concatenate([np.arange(30, 190), 200 + rng.choice(V - 200, 71,
+                                                                           replace=False)]))
+        ids = ids.astype(np.int32)
+    dev_ids = None if ids is None else torch.tensor(ids, device=DEV)
+    y = ctx.mx4_logits(h, w, keep_ids=dev_ids, planes=planes)
+    again = ctx.mx4_logits(h, w, keep_ids=dev_ids, planes=planes)
+    ctx.sync()
+    want = ora.product(f64(h), table, fmt, planes, ids)
+    assert_close(f64(y), want, product_bound(f64(h), table, fmt, planes, ids, torch.float32), "y")
+    assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("fmt", FMT)
 def test_product_rows_into_a_wider_buffer(sph, ctx, fmt):
     w, table = held(sph, ctx, 200, 96, fmt, 9)
@@ -246,10 +281,14 @@ def test_product_is_the_same_every_time(sph, ctx):
         assert torch.equal(ctx.mx4_logits(h, w, planes=3), first)
 
 
-def test_product_waits_give_up(sph):
+@pytest.mark.parametrize("pair", [1, 2])
+@pytest.mark.parametrize("schedule", [1, 2])
+def test_product_waits_give_up(sph, pair, schedule):
     # a wait limit of one cycle runs out somewhere: the call ends, sync reports
     # it, and the context works again with the limit restored
     c = sph.Context(0)
+    c.set_option(sph.SPH_OPT_TC_PAIR, pair)
+    c.set_option(sph.SPH_OPT_TC_SCHEDULE, schedule)
     w, table = held(sph, c, 4000, 4096, "e8m0", 1)
     h = make_x(64, 4096, torch.float32, 2)
     c.mx4_logits(h, w)
