@@ -37,16 +37,13 @@ def nearest(values: np.ndarray, grid: np.ndarray) -> np.ndarray:
     return np.where((d_hi < d_lo) | ((d_hi == d_lo) & (hi % 2 == 0)), hi, lo)
 
 
-def row_exponent(amax: float) -> int:
+def row_exponent(amax: np.ndarray) -> np.ndarray:
     """Least k with amax <= 2688 * 2^k, in [-110, 116]; 0 for a row of zeros."""
-    if amax == 0:
-        return 0
-    k = -400
-    m, e = np.frexp(amax / 2688.0)         # amax / 2688 = m 2^e, m in [0.5, 1)
-    for k in (int(e) - 2, int(e) - 1, int(e), int(e) + 1):
-        if amax <= 2688.0 * 2.0 ** k:
-            break
-    return int(min(116, max(-110, k)))
+    amax = np.asarray(amax, np.float64)
+    k = np.frexp(amax / 2688.0)[1].astype(np.int64) + 1      # (one too many at least)
+    for _ in range(3):
+        k = np.where(amax <= 2688.0 * 2.0 ** (k - 1.0), k - 1, k)
+    return np.where(amax > 0, np.clip(k, -110, 116), 0)
 
 
 def encode(x, fmt: str, row_exps=None):
@@ -59,30 +56,24 @@ def encode(x, fmt: str, row_exps=None):
     b = np.zeros((R, dp))
     b[:, :d] = x
     b = b.reshape(R, dp // bs, bs)
-    codes = np.zeros((R, dp // bs, bs), np.uint8)
-    scales = np.zeros((R, dp // bs), np.uint8)
+    good = np.isfinite(b).all(2)
+    b = np.where(good[:, :, None], b, 0.0)
+    amax = np.abs(b).max(2)
     exps = np.zeros(R, np.int64)
-    for r in range(R):
-        good = np.isfinite(b[r]).all(1)
-        amax = np.where(good, np.abs(np.where(np.isfinite(b[r]), b[r], 0)).max(1), 0)
-        if fmt == "e4m3":
-            exps[r] = row_exponent(amax.max()) if row_exps is None else row_exps[r]
-        for i in range(nb):
-            if not good[i]:
-                scales[r, i] = 0x7F if fmt == "e4m3" else 0xFF
-                continue
-            if fmt == "e4m3":
-                scales[r, i] = nearest(np.array([amax[i] / 6 / 2.0 ** exps[r]]), _E4M3)[0]
-                step = _E4M3[scales[r, i]] * 2.0 ** exps[r]
-            else:
-                e = max(int(np.frexp(amax[i])[1]) - 3, -126) if amax[i] > 0 else -126
-                scales[r, i] = e + 127
-                step = 2.0 ** e
-            if step > 0:
-                q = nearest(np.abs(b[r, i]) / step, E2M1)
-                codes[r, i] = q + 8 * np.signbit(b[r, i])
-            else:
-                codes[r, i] = 8 * np.signbit(b[r, i])
+    if fmt == "e4m3":
+        exps = row_exponent(amax.max(1)) if row_exps is None else np.asarray(row_exps)
+        unit = 2.0 ** exps.astype(np.float64)[:, None]
+        scales = nearest((amax / 6 / unit).reshape(-1), _E4M3).reshape(amax.shape)
+        step = _E4M3[scales] * unit
+        bad = 0x7F
+    else:
+        e = np.where(amax > 0, np.maximum(np.frexp(amax)[1].astype(np.int64) - 3, -126), -126)
+        scales, step, bad = e + 127, 2.0 ** e.astype(np.float64), 0xFF
+    ratio = np.abs(b) / np.where(step > 0, step, 1.0)[:, :, None]
+    q = np.where((step > 0)[:, :, None], nearest(ratio.reshape(-1), E2M1).reshape(b.shape), 0)
+    codes = (q + 8 * np.signbit(b)).astype(np.uint8)
+    codes[~good] = 0
+    scales = np.where(good, scales, bad).astype(np.uint8)
     return codes.reshape(R, dp), scales[:, :nb], exps
 
 

@@ -5,8 +5,11 @@
 // with X the sum of `planes` terms in the table's own format (k_mx4.cu).  Both
 // operands go to the tensor cores in 4 bits with their block scales
 // (tcgen05.mma kind::mxf4nvf4): W's rows are the MMA's M = 128, the hidden
-// states its N, and the terms of X add into the same accumulator, so a term
-// costs its MMAs and no traffic of W.
+// states its N, and all terms of X meet a stage of W, so a term costs its MMAs
+// and no traffic of W.  The first two terms add into one accumulator, the third and
+// fourth into another: an MMA drops what lies below its accumulator's 24 bits, which
+// two terms mostly fit and four do not (300 rows x 5000 ids x 4608, four terms in one
+// accumulator: 3e-6 off, in two 6e-8).
 //
 // A CTA keeps a ring of stages of 256 columns, 128 bytes of codes a row: codes by
 // TMA, W's in whole boxes where the kept ids are consecutive and four gathered
@@ -259,6 +262,8 @@ struct Params {
   int bn, row_tiles, tiles, kt; // row tiles are the fast index of a tile
   int mma_n, terms;             // an MMA's N, and MMAs a step: bn and `planes`, or (few
                                 // rows) the terms' rows one after another and 1
+  int accs, acc_cols;           // accumulators of a tile: buffers, columns of each
+  int low_col;                  // where the third and fourth term's sums start (0: none)
   int stages, stage_bytes, chunks, sf_col, sf_cols, sf_sets;
   int ranges;                   // 1: equal ranges of stages, 0: whole tiles in turn
   float* parts;                 // [unit][2][half][bn][128] of tiles that a range's end cuts
@@ -602,7 +607,7 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     auto tile_mmas = [&](int from, int to) {
       if (!wait(&acc_empty[acc], acc_phase ^ 1)) return false;
       ptx::tc_fence_after();
-      const uint32_t d = tmem + acc * p.mma_n;
+      const uint32_t d = tmem + acc * p.acc_cols;
       for (int k = from; k < to; ++k) {
         if (!wait(&sf_full[set], set_phase)) return false;
         ptx::tc_fence_after();
@@ -613,13 +618,15 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
         // steps of 64 columns, none past the last column
         const int steps = min(4, (g.d - k * kCols + 63) / 64);
         for (int t = 0; t < p.terms; ++t) {
+          const uint32_t dt = t < 2 ? d : d + p.low_col;
+          const bool add = k > from || (t > 0 && (t != 2 || p.low_col == 0));
           if (steps == 4) {
-            mma4_mx4<FMT, PAIR>(d, ad, bd, idesc, other, sfa, sfb, 4 * p.chunks, k > from || t > 0);
+            mma4_mx4<FMT, PAIR>(dt, ad, bd, idesc, other, sfa, sfb, 4 * p.chunks, add);
           } else {
             for (int j = 0; j < steps; ++j) {
               const int q = FMT == MX4_E4M3 ? j : j / 2;
-              mma_mx4<FMT, PAIR>(d, ad + 2 * j, bd + 2 * j, FMT == MX4_E8M0 && j % 2 ? other : idesc,
-                                 sfa + 4 * q, sfb + q * p.chunks * 4, k > from || t > 0 || j > 0);
+              mma_mx4<FMT, PAIR>(dt, ad + 2 * j, bd + 2 * j, FMT == MX4_E8M0 && j % 2 ? other : idesc,
+                                 sfa + 4 * q, sfb + q * p.chunks * 4, add || j > 0);
             }
           }
           sfb += kGroups * p.chunks * 4;
@@ -630,8 +637,7 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
         next_set();
       }
       commit(&acc_full[acc]);
-      acc ^= 1;
-      if (acc == 0) acc_phase ^= 1;
+      if (++acc == p.accs) { acc = 0; acc_phase ^= 1; }
       return true;
     };
     if (p.ranges) {
@@ -690,7 +696,7 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       if (p.ranges) ok = all_of(1, 128, ok);
       if (!ok) break;
       ptx::tc_fence_after();
-      const uint32_t t = tmem + acc * p.mma_n + ((uint32_t)(quarter * 32) << 16);
+      const uint32_t t = tmem + acc * p.acc_cols + ((uint32_t)(quarter * 32) << 16);
       const bool whole = k0 == 0 && k1 == p.kt;
       const int64_t part_size = (int64_t)kHalves * p.bn * kM;
       // (slot 0 of a unit: the tile its range begins in)
@@ -702,7 +708,7 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
         if (32 * m >= rows) break;
         float v[32];
         ptx::tmem_ld32(t + 32 * m, v);
-        for (int c = p.bn; c < p.mma_n; c += p.bn) {     // the further terms' columns
+        for (int c = p.bn; c < p.acc_cols; c += p.bn) {  // the further terms' columns
           float w[32];
           ptx::tmem_ld32(t + c + 32 * m, w);
 #pragma unroll
@@ -719,8 +725,7 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) arrive(&acc_empty[acc]);
-      acc ^= 1;
-      if (acc == 0) acc_phase ^= 1;
+      if (++acc == p.accs) { acc = 0; acc_phase ^= 1; }
       if (!whole) {
         // the unit that counts in last adds the tile's parts
         const long long first = (long long)tile * p.kt;
@@ -807,28 +812,39 @@ bool byte_map(CUtensorMap* m, const void* ptr, uint64_t bytes, uint64_t rows, ui
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct Plan {
-  int pair, bn, mma_n, terms, row_tiles, tiles, kt, stages, stage_bytes, chunks, sf_col, sf_cols, sf_sets;
+  int pair, bn, mma_n, terms, accs, acc_cols, low_col, row_tiles, tiles, kt, stages, stage_bytes, chunks, sf_col, sf_cols, sf_sets;
   int units, ranges;
 };
 int stage_bytes_of(int bn, int planes, int fmt, int pair) {
   const int x = planes * bn / (pair ? 2 : 1) * (kCols / 2);
   return (kABytes + x + planes * bn * groups_of(fmt) * 4 + 1023) / 1024 * 1024;
 }
-int sf_col_of(int bn) { return (2 * bn + 31) / 32 * 32; }
+int sf_col_of(int acc_cols, int accs) { return (accs * acc_cols + 31) / 32 * 32; }
 int sf_cols_of(int bn, int planes, int fmt) {
   return 4 * groups_of(fmt) * (1 + planes * ((bn + 127) / 128));
 }
 constexpr int kExtraBytes = 1024 + kBarBytes + kWsSlots * kWsBytes;   // beside the stages
-// Whether tiles of bn rows fit: three stages, two accumulators and two sets of scales.
-bool fits(int bn, int planes, int fmt, int pair, bool stacked) {
+// Columns of an accumulator: the rows' (stacked: the terms' one after another), twice
+// from three terms on.
+int acc_cols_of(int bn, int planes, bool stacked) {
+  return stacked ? planes * bn : planes > 2 ? 2 * bn : bn;
+}
+// Whether tiles of bn rows fit: three stages, `accs` accumulators and two sets of scales.
+bool fits(int bn, int planes, int fmt, int pair, bool stacked, int accs) {
   const int n = stacked ? planes * bn : bn;
-  return n <= 256 && 3 * stage_bytes_of(bn, planes, fmt, pair) + kExtraBytes <= kSmemMax &&
-         sf_col_of(n) + 2 * sf_cols_of(n, stacked ? 1 : planes, fmt) <= (int)kTmemCols;
+  return n <= kMaxBn && 3 * stage_bytes_of(bn, planes, fmt, pair) + kExtraBytes <= kSmemMax &&
+         sf_col_of(acc_cols_of(bn, planes, stacked), accs) +
+                 2 * sf_cols_of(n, stacked ? 1 : planes, fmt) <= (int)kTmemCols;
+}
+int largest(int unit, int planes, int fmt, int pair, int accs) {
+  int most = unit;
+  for (int bn = unit; bn <= kMaxBn && fits(bn, planes, fmt, pair, false, accs); bn += unit) most = bn;
+  return most;
 }
 // The largest tile of hidden-state rows that fits, then as many equal tiles as the rows
 // need.  Pairs where several terms make X's codes the larger part of a stage (single CTAs
-// / pairs, us: 1024 rows x 38912 ids x 4608, one term 97.5 / 107, two 158 / 140, four 333 /
-// 229; 320 x 51302 x 3584, two terms 72.7 / 70.5; 100 x 20000 x 2000, three 24.1 / 20.6;
+// / pairs, us: 1024 rows x 38912 ids x 4608, one term 97.5 / 107, two 158 / 140, four 372 /
+// 260; 320 x 51302 x 3584, two terms 72.3 / 70.9; 100 x 20000 x 2000, three 25.7 / 22.8;
 // 32 x 12000 x 3840, two, with the terms side by side, 12.3 / 13.4).  On pairs a tile of
 // more than 128 rows, whose scales take twice the columns, costs a third more a stage:
 // it is taken only where that saves more (the 1024 rows, two terms, in 8 tiles of 128 140
@@ -838,15 +854,24 @@ Plan plan_of(const Mx4Plan& a) {
   pl.pair = a.pair_units > 0 &&
             (a.pair_mode == 2 || (a.pair_mode == 1 && a.planes > 1 && a.rows > kPairRows));
   const int unit = pl.pair ? 32 : 16;         // rows a tile is a multiple of
-  int most = unit;
-  for (int bn = unit; bn <= kMaxBn && fits(bn, a.planes, a.fmt, pl.pair, false); bn += unit) most = bn;
+  // two accumulators, so that a tile is stored while the next is computed; one where
+  // that halves the tile's rows (three and four terms of more rows than fit so)
+  pl.accs = 2;
+  int most = largest(unit, a.planes, a.fmt, pl.pair, 2);
+  if (a.planes > 2 && a.rows > most) {
+    pl.accs = 1;
+    most = largest(unit, a.planes, a.fmt, pl.pair, 1);
+  }
   int64_t count = (a.rows + most - 1) / most;
   if (pl.pair && most > 128 && (a.rows + 127) / 128 * 3 < count * 4) count = (a.rows + 127) / 128;
   pl.bn = (int)(((a.rows + count - 1) / count + unit - 1) / unit * unit);
   // one row tile whose terms fit side by side: one MMA a step instead of one a term
   // (not on pairs, whose CTAs hold half of an MMA's columns each)
   const bool stacked =
-      a.planes > 1 && count == 1 && !pl.pair && fits(pl.bn, a.planes, a.fmt, pl.pair, true);
+      a.planes > 1 && count == 1 && !pl.pair && fits(pl.bn, a.planes, a.fmt, 0, true, 2);
+  if (stacked) pl.accs = 2;
+  pl.acc_cols = acc_cols_of(pl.bn, a.planes, stacked);
+  pl.low_col = !stacked && a.planes > 2 ? pl.bn : 0;
   pl.mma_n = stacked ? a.planes * pl.bn : pl.bn;
   pl.terms = stacked ? 1 : a.planes;
   pl.row_tiles = (int)((a.rows + pl.bn - 1) / pl.bn);
@@ -857,7 +882,7 @@ Plan plan_of(const Mx4Plan& a) {
   pl.stages = (kSmemMax - kExtraBytes) / pl.stage_bytes;
   if (pl.stages > kMaxStages) pl.stages = kMaxStages;
   pl.chunks = (pl.mma_n + 127) / 128;
-  pl.sf_col = sf_col_of(pl.mma_n);
+  pl.sf_col = sf_col_of(pl.acc_cols, pl.accs);
   pl.sf_cols = sf_cols_of(pl.mma_n, pl.terms, a.fmt);
   pl.sf_sets = ((int)kTmemCols - pl.sf_col) / pl.sf_cols;
   if (pl.sf_sets > kMaxSets) pl.sf_sets = kMaxSets;
@@ -955,6 +980,7 @@ cudaError_t launch_mx4_gemm(const Mx4Gemm& g, const Mx4Plan& a, void* scratch, l
   p.stages = pl.stages; p.stage_bytes = pl.stage_bytes; p.chunks = pl.chunks;
   p.sf_col = pl.sf_col; p.sf_cols = pl.sf_cols; p.sf_sets = pl.sf_sets;
   p.ranges = pl.ranges; p.mma_n = pl.mma_n; p.terms = pl.terms;
+  p.accs = pl.accs; p.acc_cols = pl.acc_cols; p.low_col = pl.low_col;
   p.counts = reinterpret_cast<unsigned*>(at + o.counts);
   p.parts = reinterpret_cast<float*>(at + o.parts);
   p.spin_limit = spin_limit;

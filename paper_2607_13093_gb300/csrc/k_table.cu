@@ -601,9 +601,10 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
     const int32_t t = __shfl_sync(0xFFFFFFFFu, q < 32 ? at : next_at, q & 31);
     return static_cast<const T*>(a.d_out) + (int64_t)t * a.ld_d_out;
   };
+  const bool inside = col + 8 <= a.d;
   auto copy16 = [&](uint4* dst, const void* row, int q, int size) {
     // columns past the row's last are zeros, and not read
-    const int bytes = min(16, max(0, (a.d - col) * size - 16 * q));
+    const int bytes = inside ? 16 : min(16, max(0, (a.d - col) * size - 16 * q));
     if (active)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)),
                    "l"(static_cast<const uint4*>(row) + (bytes > 0 ? q : 0)), "r"(bytes)

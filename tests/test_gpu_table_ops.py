@@ -417,6 +417,48 @@ def test_gradient_of_skewed_tokens(sph, ctx, case, T):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("seed", range(6))
+@pytest.mark.parametrize("d,src,out", [(40, torch.bfloat16, torch.float32),
+                                       (1032, torch.float32, torch.bfloat16),
+                                       (33, torch.bfloat16, torch.bfloat16)])
+@pytest.mark.parametrize("add", [False, True])
+def test_gradient_of_random_runs(sph, ctx, seed, d, src, out, add):
+    # runs of equal ids of every length around the ranges' and the windows' (1 to 140),
+    # some ids absent, the tokens shuffled
+    rng = np.random.default_rng(seed)
+    lengths = rng.choice([1, 2, 7, 8, 9, 15, 16, 17, 18, 31, 32, 33, 34, 64, 65, 140],
+                         int(rng.integers(20, 90)))
+    ids = np.sort(rng.choice(4000, len(lengths), replace=False))
+    tok = rng.permutation(np.concatenate([np.repeat(ids, lengths), np.full(rng.integers(0, 40), -1)]))
+    d_out = torch.tensor(rng.standard_normal((len(tok), d)), dtype=src, device=DEV)
+    onto = torch.tensor(rng.standard_normal((4000, d)), dtype=out, device=DEV) if add else \
+        torch.full((4000, d), float("nan"), dtype=out, device=DEV)
+    start = f64(onto)
+    got = ctx.embed_grad(torch.tensor(tok, dtype=torch.int32, device=DEV), d_out, 4000, scale=0.75,
+                         accumulate=add, out=onto)
+    ctx.sync()
+    base = start if add else None
+    want = ora.gradient(tok, f64(d_out), 4000, 0.75, onto=base)
+    assert_close(f64(got), want, grad_bound(tok, f64(d_out), 4000, 0.75, out, base), "runs")
+
+
+@pytest.mark.parametrize("V,d,T", [(300000, 128, 3000), (99991, 257, 1), (70001, 1024, 9000)])
+def test_gradient_fills_every_row_of_a_large_table(sph, ctx, V, d, T):
+    # (rows beyond the ones zeroed beside the sort: over 96 MB)
+    rng = np.random.default_rng(V)
+    tok = rng.integers(0, V, T)
+    tok[0] = V - 1
+    d_out = torch.tensor(rng.standard_normal((T, d)), dtype=torch.float32, device=DEV)
+    out = torch.full((V, d), float("nan"), device=DEV)
+    t = torch.tensor(tok, device=DEV)
+    ctx.embed_grad(t.int(), d_out, V, out=out)
+    ctx.sync()
+    want = torch.zeros(V, d, dtype=torch.float64, device=DEV).index_add_(0, t, d_out.double())
+    n = int(np.bincount(tok).max())
+    mag = torch.zeros(V, d, dtype=torch.float64, device=DEV).index_add_(0, t, d_out.double().abs())
+    assert bool(((out.double() - want).abs() <= (n + 2) * 2.0 ** -24 * 1.01 * mag).all())
+
+
 def test_gradient_of_long_lists(sph, ctx):
     # more tokens than the cluster's tiles hold, over ids that need four digits
     T, d, V = 150000, 8, 300_000_007
@@ -473,6 +515,72 @@ def test_gradient_against_differences(sph, ctx):
             hi[v, c] += 1e-3
             diff = ((f64(C32) * (ora.lookup(tok, hi, 2.0) - ora.lookup(tok, lo, 2.0))).sum()) / 2e-3
             assert abs(got[v, c] - diff) < 1e-5
+
+
+# ---- offsets past 32 bits, tiny tables ---------------------------------------------
+def test_offsets_past_32_bits(sph, ctx):
+    V, d = 600_000, 8192                  # 4.9e9 elements; 2.5e9 bytes of codes
+    rng = np.random.default_rng(1)
+    ids = np.array([0, 5, 262143, 262144, 524288, V - 3, V - 1], np.int32)
+    t = torch.tensor(ids, device=DEV)
+    rows = make_x(len(ids), d, torch.bfloat16, 3)
+    table = torch.zeros(V, d, dtype=torch.bfloat16, device=DEV)
+    table[t.long()] = rows
+    assert torch.equal(ctx.embed(t, table), rows)
+    got = ctx.embed_grad(t, rows, V, out=table, accumulate=True)
+    ctx.sync()
+    assert torch.equal(got[t.long()], (rows.float() * 2).bfloat16())
+    del table, got
+    w = sph.mx4_empty(V, d, sph.SPH_MX4_E4M3, DEV)
+    few = ctx.mx4_quantize(rows, sph.SPH_MX4_E4M3)
+    for dst, src in zip(w[:3], few[:3]):
+        dst.zero_()
+        dst[t.long()] = src
+    values = decoded(few, "e4m3")
+    assert np.array_equal(f64(ctx.embed(t, w, dtype=torch.float32)), values)
+    h = make_x(3, d, torch.float32, 4)
+    for keep in (t, None):
+        y = ctx.mx4_logits(h, w, keep_ids=keep, planes=2)
+        y = y if keep is not None else y[:, t.long()]
+        want = ora.product(f64(h), values, "e4m3", 2)
+        assert_close(f64(y), want, product_bound(f64(h), values, "e4m3", 2, None, torch.float32), "y")
+    big = torch.zeros(1 << 20, 2304, dtype=torch.bfloat16, device=DEV)       # 2.4e9 elements
+    big[-1] = 1
+    back = ctx.mx4_dequantize(ctx.mx4_quantize(big))
+    ctx.sync()
+    ones = ora.decode(*ora.encode(np.ones((1, 2304)), "e4m3"), 2304, "e4m3")
+    assert np.array_equal(f64(back[-1:]), ones) and float(back[:-1].abs().max()) == 0
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("V,keep", [(5, [1, 3]), (1, [0]), (33, list(range(33))), (40, [39])])
+def test_product_of_tiny_tables(sph, ctx, fmt, V, keep):
+    w, table = held(sph, ctx, V, 48, fmt, V)
+    h = make_x(2, 48, torch.float32, 1)
+    y = ctx.mx4_logits(h, w, keep_ids=torch.tensor(keep, dtype=torch.int32, device=DEV))
+    ctx.sync()
+    want = ora.product(f64(h), table, fmt, 2, np.array(keep))
+    assert_close(f64(y), want,
+                 product_bound(f64(h), table, fmt, 2, np.array(keep), torch.float32), "y")
+
+
+def test_calls_between_the_other_ones(sph, ctx):
+    # the context's scratch goes from call to call without a wait between
+    w, _ = held(sph, ctx, 3000, 512, "e4m3", 1)
+    table = make_x(3000, 512, torch.bfloat16, 2)
+    h = make_x(64, 512, torch.float32, 3)
+    tok = torch.randint(0, 3000, (5000,), dtype=torch.int32, device=DEV)
+    d_out = make_x(5000, 512, torch.bfloat16, 4)
+    alone = []
+    for call in (lambda: ctx.mx4_logits(h, w), lambda: ctx.embed_grad(tok, d_out, 3000),
+                 lambda: ctx.partial_logits(h, table)[0], lambda: ctx.mx4_logits(h[:1], w, planes=4)):
+        alone.append((call, call().clone()))
+        torch.cuda.synchronize()
+    for _ in range(20):
+        got = [call() for call, _ in alone]
+    torch.cuda.synchronize()
+    for g, (_, want) in zip(got, alone):
+        assert torch.equal(g, want)
 
 
 # ---- streams, capture, refusals -------------------------------------------------------
