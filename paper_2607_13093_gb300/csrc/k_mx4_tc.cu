@@ -34,6 +34,7 @@
 #include <cuda_bf16.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "mx4.cuh"
 #include "sm100_ptx.cuh"
@@ -94,8 +95,8 @@ __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[N]) 
 // tensor memory: word q of row r goes to lane r % 32 of column q * 4 C + r / 32.
 // (What rows past `rows` get is read by no MMA.)
 template <int G, int C>
-__device__ __forceinline__ void put_scales(uint32_t taddr, const uint8_t* src, int rows, int lane) {
-  uint32_t w[G * 4 * C];
+__device__ __forceinline__ void load_scales(uint32_t (&w)[G * 4 * C], const uint8_t* src, int rows,
+                                            int lane) {
 #pragma unroll
   for (int i = 0; i < 4 * C; ++i) {
     uint4 v = make_uint4(0, 0, 0, 0);
@@ -115,12 +116,11 @@ __device__ __forceinline__ void put_scales(uint32_t taddr, const uint8_t* src, i
       w[12 * C + i] = v.w;
     }
   }
-  tmem_st(taddr, w);
 }
 // W's, from the 64-byte rows of several stages (kWsRow).
 template <int G>
-__device__ __forceinline__ void put_w_scales(uint32_t taddr, const uint8_t* src, int in_slot, int lane) {
-  uint32_t w[G * 4];
+__device__ __forceinline__ void load_w_scales(uint32_t (&w)[G * 4], const uint8_t* src, int in_slot,
+                                              int lane) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = 32 * i + lane, piece = G == 4 ? in_slot : in_slot / 2;
@@ -133,7 +133,6 @@ __device__ __forceinline__ void put_w_scales(uint32_t taddr, const uint8_t* src,
       w[i] = v.x; w[4 + i] = v.y;
     }
   }
-  tmem_st(taddr, w);
 }
 // e2m1 operands, K-major, fp32 accumulator: N, M / 16, and the scales' format
 // (bit 23: e8m0).  With 32-column blocks an MMA's two scales are the low or the
@@ -478,12 +477,12 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       }
     }
   } else if (warp == kWarpX) {
-    // ---- X codes -----------------------------------------------------------
-    // (One copy for all terms: each one that a producer's thread issues takes it some
-    // 150 cycles.)
+    // ---- X codes and scales ------------------------------------------------
+    // (One copy each for all terms: each one that a producer's thread issues takes it
+    // some 150 cycles.)
     ptx::griddep_wait();
     while (ok && work.next(tile, k0, k1)) {
-      const int r0 = tile % p.row_tiles * p.bn + half * bnc;
+      const int rt = tile % p.row_tiles, r0 = rt * p.bn + half * bnc;
       for (int k = k0; k < k1; ++k) {
         if (!wait(&empty[stage], phase ^ 1)) { ok = false; break; }
         if (lane == 0) {
@@ -493,14 +492,18 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
             ptx::tma_load_3d_pair(s, &map_x, k * (kCols / 2), r0, 0, leader(&full[stage]));
           else
             ptx::tma_load_3d(s, &map_x, k * (kCols / 2), r0, 0, &full[stage]);
+          const uint32_t size = (uint32_t)(g.planes * xs_bytes);
+          ptx::mbar_expect_tx(&raw[stage], size);
+          bulk_load(s - kABytes + off_xs, p.x_scales + ((int64_t)rt * p.kt + k) * size, size,
+                    &raw[stage]);
         }
         __syncwarp();
         advance();
       }
     }
   } else if (warp == kWarpRaw) {
-    // ---- scales to shared memory -------------------------------------------
-    // X's by one copy a stage, W's by cp.async, 64 bytes a row (four or eight stages' worth) by four lanes, so that
+    // ---- W scales to shared memory -----------------------------------------
+    // By cp.async, 64 bytes a row (four or eight stages' worth) by four lanes, so that
     // an instruction touches 8 rows.  (16 bytes of 32 rows an instruction cost the
     // shared memory some 50 cycles each, a quarter of what a stage has; boxes of 16
     // bytes by 128 rows by TMA took longer still.)  The 16-byte piece c of row r lies
@@ -508,46 +511,34 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     // twice.  Rows past the last kept id and bytes past the last scale become zeros.
     const int bytes = (g.d + Mx4<FMT>::kBlock - 1) / Mx4<FMT>::kBlock;
     const int sub = lane >> 2, piece = lane & 3;
-    ptx::griddep_wait();
     int slot = 0;
     uint32_t slot_phase = 0;
     while (ok && work.next(tile, k0, k1)) {
-      const int rt = tile % p.row_tiles, j0 = first_row(tile) + sub;
+      const int j0 = first_row(tile) + sub;
       int id[kM / 8];
 #pragma unroll
       for (int i = 0; i < kM / 8; ++i) {
         const int j = j0 + 8 * i;
         id[i] = j < g.n ? (GATHER ? g.ids[j] : j) : -1;
       }
-      for (int k = k0; k < k1; ++k) {
-        if (k == k0 || k % kWsStages == 0) {
-          if (!wait(&ws_empty[slot], slot_phase ^ 1)) { ok = false; break; }
-          const int at = k / kWsStages * kWsRow + 16 * piece, left = min(16, max(0, bytes - at));
-          const uint32_t dst = ptx::smem_u32(ws_ring + slot * kWsBytes);
+      for (int w = k0 / kWsStages; w * kWsStages < k1; ++w) {
+        if (!wait(&ws_empty[slot], slot_phase ^ 1)) { ok = false; break; }
+        const int at = w * kWsRow + 16 * piece, left = min(16, max(0, bytes - at));
+        const uint32_t dst = ptx::smem_u32(ws_ring + slot * kWsBytes);
 #pragma unroll
-          for (int i = 0; i < kM / 8; ++i) {
-            const int r = 8 * i + sub;
-            const bool there = id[i] >= 0 && left > 0;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                             dst + r * kWsRow + (piece ^ (r >> 1 & 3)) * 16),
-                         "l"(there ? g.w_scales + (int64_t)id[i] * g.ld_scales + at : g.w_scales),
-                         "r"(there ? left : 0)
-                         : "memory");
-          }
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(
-                           ptx::smem_u32(&ws_full[slot]))
+        for (int i = 0; i < kM / 8; ++i) {
+          const int r = 8 * i + sub;
+          const bool there = id[i] >= 0 && left > 0;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                           dst + r * kWsRow + (piece ^ (r >> 1 & 3)) * 16),
+                       "l"(there ? g.w_scales + (int64_t)id[i] * g.ld_scales + at : g.w_scales),
+                       "r"(there ? left : 0)
                        : "memory");
-          if (++slot == kWsSlots) { slot = 0; slot_phase ^= 1; }
         }
-        if (!wait(&empty[stage], phase ^ 1)) { ok = false; break; }
-        if (lane == 0) {
-          const uint32_t size = (uint32_t)(g.planes * xs_bytes);
-          ptx::mbar_expect_tx(&raw[stage], size);
-          bulk_load(base + (size_t)stage * p.stage_bytes + off_xs,
-                    p.x_scales + ((int64_t)rt * p.kt + k) * size, size, &raw[stage]);
-        }
-        __syncwarp();
-        advance();
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(
+                         ptx::smem_u32(&ws_full[slot]))
+                     : "memory");
+        if (++slot == kWsSlots) { slot = 0; slot_phase ^= 1; }
       }
     }
   } else if ((warp >= kWarpScale && warp < kWarpScale + 4) || warp >= kWarpScale2) {
@@ -567,20 +558,30 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
         const int in_slot = k % kWsStages;
         if ((k == k0 || in_slot == 0) && !wait(&ws_full[slot], slot_phase)) { ok = false; break; }
         if (turn) {
-          if (!wait(&raw[stage], phase) || (behind >= 0 && !wait(&empty[had], had_phase))) {
+          if (!wait(&raw[stage], phase)) { ok = false; break; }
+          // (in registers before the set is free: what comes after that delays the MMAs)
+          uint32_t w[4 * kGroups];
+          load_w_scales<kGroups>(w, ws_ring + slot * kWsBytes, in_slot, lane);
+          const uint8_t* xs = base + (size_t)stage * p.stage_bytes + off_xs;
+          const uint32_t to = tmem + lanes + p.sf_col + set * p.sf_cols;
+          auto move = [&](auto chunks) {
+            constexpr int C = decltype(chunks)::value;
+            uint32_t x[4 * kGroups * C];
+            load_scales<kGroups, C>(x, xs, p.mma_n, lane);
+            if (behind >= 0 && !wait(&empty[had], had_phase)) return false;
+            ptx::tc_fence_after();
+            tmem_st(to, w);
+            tmem_st(to + 4 * kGroups, x);
+            for (int t = 1; t < p.terms; ++t) {
+              load_scales<kGroups, C>(x, xs + t * p.mma_n * kRow, p.mma_n, lane);
+              tmem_st(to + 4 * kGroups * (1 + t * C), x);
+            }
+            return true;
+          };
+          if (!(p.chunks == 1 ? move(std::integral_constant<int, 1>())
+                              : move(std::integral_constant<int, 2>()))) {
             ok = false;
             break;
-          }
-          ptx::tc_fence_after();
-          uint32_t to = tmem + lanes + p.sf_col + set * p.sf_cols;
-          put_w_scales<kGroups>(to, ws_ring + slot * kWsBytes, in_slot, lane);
-          to += 4 * kGroups;
-          const uint8_t* xs = base + (size_t)stage * p.stage_bytes + off_xs;
-          const int term_bytes = p.mma_n * kRow;
-          for (int t = 0; t < p.terms; ++t) {
-            if (p.chunks == 1) put_scales<kGroups, 1>(to, xs + t * term_bytes, p.mma_n, lane);
-            else put_scales<kGroups, 2>(to, xs + t * term_bytes, p.mma_n, lane);
-            to += kGroups * p.chunks * 4;
           }
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           ptx::tc_fence_before();
