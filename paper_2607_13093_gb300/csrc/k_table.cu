@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const Lookup a) {
   const int first = (int)(blockIdx.x % a.blocks) * a.turns * kLookSpan +
                     (VEC ? (int)threadIdx.x * 8 : (int)threadIdx.x);
   const int64_t id = a.tokens ? a.tokens[t] : t;
-  const bool there = id >= 0 && id < a.V;
+  const bool there = id >= 0 && id < a.V && id != a.padding;
   if (!there && id != a.padding && first == 0) atomicOr(a.status, ERR_BAD_INDEX);
   const float row = FMT == MX4_E4M3 && there ? a.row_scale[id] : 1.f;
   OT* out = static_cast<OT*>(a.out) + t * a.ld_out;
@@ -165,9 +165,11 @@ __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const Lookup a) {
 
 template <class TT, int FMT, class OT, bool VEC>
 cudaError_t launch_lookup_v(Lookup a, int sm_count, cudaStream_t st) {
-  // one block a token once that gives every SM sixteen, else a block for each span
+  // One block a token once that gives every SM two, else a block for each span
+  // (a block a token / a span, us, into bf16: 32 tokens x 5120 from e4m3 2.8 / 2.4, 500
+  // 3.5 / 4.1, 1200 4.5 / 7.4; 32 x 4096 from bf16 3.1 / 2.5, 500 3.7 / 3.6, 1200 4.6 / 6.2).
   const int spans = (a.d + kLookSpan - 1) / kLookSpan;
-  a.turns = a.n >= (int64_t)sm_count * 16 ? spans : 1;
+  a.turns = a.n >= (int64_t)sm_count * 2 ? spans : 1;
   a.blocks = (spans + a.turns - 1) / a.turns;
   const dim3 grid((unsigned)(a.n * a.blocks));
   if (a.turns > 4 && FMT >= 0)          // (4-bit pieces are two registers each)
@@ -213,13 +215,14 @@ struct SortSmem {
 };
 
 // One cluster sorts: stable radix passes over (id, position) with digits of at most
-// 9 bits, each CTA a contiguous part.  A warp's items are consecutive; equal
-// digits within a warp are ranked by votes, its warps by a prefix over their counts, the CTAs by one over theirs, read through distributed shared memory.
+// 9 bits, each CTA a contiguous part.  A warp's items are consecutive; equal digits
+// within a warp are ranked by votes, its warps by a prefix over their counts, the CTAs
+// by one over theirs, read through distributed shared memory.
 // A tile is put in order in shared memory first and written from there, a digit's
 // elements side by side (one by one from the ranking, 8000 tokens took 24 us).  Up
 // to kSortTile tokens (one CTA) the passes stay in shared memory; parts of one tile
 // get their counts from the ranking, longer ones from a pass of their own.
-// Ids out of range become V, which sorts last.
+// The padding id and ids out of range become V, which sorts last.
 // FIRST: the call's first kernel.  Else it runs beside the one that zeroes rows, and
 // waits for that only at its end, so that the kernel after it may take both as done.
 template <bool FIRST>
@@ -243,7 +246,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
     auto key_of = [&](int i) {
       if (pass > 0) return __ldcg(a.keys[to ^ 1] + i);
       const int32_t id = a.tokens[i];
-      return id >= 0 && id < a.V ? id : a.V;
+      return id >= 0 && id < a.V && id != a.padding ? id : a.V;
     };
     auto digit = [&](int32_t k) { return (int)((uint32_t)k >> shift) & (bins - 1); };
     // exclusive sum over the block's threads (thread b: digit b)
@@ -324,7 +327,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
       if (pass == 0) {
 #pragma unroll
         for (int i = 0; i < kSortItems; ++i) {
-          const bool out = k[i] < 0 || k[i] >= a.V;
+          const bool out = k[i] < 0 || k[i] >= a.V || k[i] == a.padding;
           if (out && k[i] != a.padding && p[i] >= 0) atomicOr(a.status, ERR_BAD_INDEX);
           if (out) k[i] = a.V;
         }
@@ -417,7 +420,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
 // gradient: zero rows
 // ---------------------------------------------------------------------------
 constexpr int kFillThreads = 512, kFillIds = 8192;
-constexpr int64_t kHeadBytes = 96 << 20;      // rows zeroed while the sort runs
 
 // Zeros, by one warp, over bytes of any alignment.
 __device__ __forceinline__ void zero_bytes(uint8_t* p, int64_t bytes, int lane) {
@@ -431,17 +433,17 @@ __device__ __forceinline__ void zero_bytes(uint8_t* p, int64_t bytes, int lane) 
   if (done + 2 * lane < bytes) *reinterpret_cast<uint16_t*>(p + done + 2 * lane) = 0;
 }
 
-// Block `b` of `blocks` zeroes the rows of its share of the ids v_from .. v_to - 1 that
+// Block `b` of `blocks` zeroes the rows of its share of the ids 0 .. V - 1 that
 // no token has: it marks the ones that occur from the whole token list (a read of
 // the L2, once per kFillIds ids), so nothing is written twice.
-__device__ __forceinline__ void zero_rows(const TableGrad& a, int64_t v_from, int64_t v_to, int b,
+__device__ __forceinline__ void zero_rows(const TableGrad& a, int b,
                                           int blocks, int elem, uint32_t* s_seen) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t v0 = v_from + (v_to - v_from) * b / blocks;
-  const int64_t v1 = v_from + (v_to - v_from) * (b + 1) / blocks;
+  const int64_t v0 = (int64_t)a.V * b / blocks;
+  const int64_t v1 = (int64_t)a.V * (b + 1) / blocks;
   auto mark = [&](int32_t token, int64_t base, int ids) {
     const int64_t r = (int64_t)token - base;
-    if (r >= 0 && r < ids) atomicOr(&s_seen[r >> 5], 1u << (r & 31));
+    if (r >= 0 && r < ids && token != a.padding) atomicOr(&s_seen[r >> 5], 1u << (r & 31));
   };
   // (tokens on 16 bytes: four to a load, and four loads on their way)
   const int quads = ((uintptr_t)a.tokens & 15) == 0 ? a.n / 4 : 0;
@@ -474,19 +476,20 @@ __device__ __forceinline__ void zero_rows(const TableGrad& a, int64_t v_from, in
   }
 }
 
-// The call's first kernel where it zeroes rows: the sort runs beside it, so it takes
-// about as many rows as the sort takes time, ids 0 .. v_to - 1.
-__global__ void __launch_bounds__(kFillThreads) head_kernel(const TableGrad a, int elem, int64_t v_to) {
+// The call's first kernel where it zeroes rows; the sort runs beside it.  (All rows
+// here / 96 MB of them here and the rest beside the joins, us: 32768 tokens into 128256
+// x 4096 bf16 228 / 238, 4000 172 / 176; 500 into 32000 x 4096 fp32 91.5 / 90.2.)
+__global__ void __launch_bounds__(kFillThreads) head_kernel(const TableGrad a, int elem) {
   __shared__ uint32_t s_seen[kFillIds / 32];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  zero_rows(a, 0, v_to, (int)blockIdx.x, (int)gridDim.x, elem, s_seen);
+  zero_rows(a, (int)blockIdx.x, (int)gridDim.x, elem, s_seen);
 }
 
 // ---------------------------------------------------------------------------
 // gradient: sums over ranges of sorted positions, and the join
 // ---------------------------------------------------------------------------
-constexpr int kSumThreads = 128;
+constexpr int kSumThreads = 128, kJoinThreads = 512;
 constexpr int kSumBytes = 256;      // shared memory of a thread: rows requested ahead
 constexpr int kShortRun = 16;       // (at most 32) positions of a run that one range takes whole
 
@@ -702,26 +705,18 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
     a.keys[1][atomicAdd(&a.pos[1][0], 1)] = (int32_t)r;
 }
 
-// The last kernel.  Its first `joins` blocks add up the runs that cross ranges, from
-// the list that the sums left (in any order: each is summed by itself); the others
-// zero the rows of ids v_from .. V - 1 meanwhile.  A run's parts (slot 2 r + 1 of the
+// The last kernel: adds up the runs that cross ranges, from the list that the sums
+// left (in any order: each is summed by itself).  A run's parts (slot 2 r + 1 of the
 // range r it begins in, then slot 2 j of the ranges j it reaches) are shared by the
 // block's thread groups in contiguous shares, which are added in order.
 template <class OT, bool VEC>
-__global__ void __launch_bounds__(kFillThreads) tail_kernel(const TableGrad a, int ct, int joins,
-                                                            int64_t v_from) {
-  constexpr int kJoinThreads = kFillThreads;
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const TableGrad a, int ct) {
   __shared__ float s_sum[kJoinThreads * 8];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  if ((int)blockIdx.x >= joins) {
-    zero_rows(a, v_from, a.V, (int)blockIdx.x - joins, (int)gridDim.x - joins, (int)sizeof(OT),
-              reinterpret_cast<uint32_t*>(s_sum));
-    return;
-  }
   const int32_t* keys = a.keys[0];
   const int64_t work = (int64_t)a.pos[1][0] * a.groups;
-  for (int64_t item = blockIdx.x; item < work; item += joins) {
+  for (int64_t item = blockIdx.x; item < work; item += gridDim.x) {
     const int group = (int)(item % a.groups);
     const int64_t r = a.keys[1][item / a.groups];
     const int32_t id = keys[(r + 1) * a.range];
@@ -767,7 +762,7 @@ __global__ void __launch_bounds__(kFillThreads) tail_kernel(const TableGrad a, i
 }
 
 template <class T, class OT, bool VEC>
-cudaError_t launch_sums(const TableGrad& a, int ct, int64_t v_from, int sm_count, cudaStream_t st) {
+cudaError_t launch_sums(const TableGrad& a, int ct, int sm_count, cudaStream_t st) {
   const int64_t ranges = (a.n + (int64_t)a.range - 1) / a.range;
   const int per = kSumThreads / ct;
   cudaError_t e = launch_pdl(a.add ? sum_kernel<T, OT, VEC, true> : sum_kernel<T, OT, VEC, false>,
@@ -776,23 +771,21 @@ cudaError_t launch_sums(const TableGrad& a, int ct, int64_t v_from, int sm_count
   if (e != cudaSuccess) return e;
   const int64_t most = (ranges - 1) * a.groups, grid = 2 * (int64_t)sm_count;
   const int joins = a.n <= kShortRun ? 0 : (int)(most < grid ? most : grid);
-  const int zeros = v_from < a.V ? 2 * sm_count : 0;
-  if (joins + zeros == 0) return e;
-  return launch_pdl(tail_kernel<OT, VEC>, dim3((unsigned)(joins + zeros)), dim3(kFillThreads), 0, st,
-                    a, ct, joins, v_from);
+  if (joins == 0) return e;
+  return launch_pdl(join_kernel<OT, VEC>, dim3((unsigned)joins), dim3(kJoinThreads), 0, st, a, ct);
 }
 template <class T, class OT>
-cudaError_t launch_sums_v(const TableGrad& a, int ct, bool vec, int64_t v_from, int sm_count,
+cudaError_t launch_sums_v(const TableGrad& a, int ct, bool vec, int sm_count,
                           cudaStream_t st) {
-  return vec ? launch_sums<T, OT, true>(a, ct, v_from, sm_count, st)
-             : launch_sums<T, OT, false>(a, ct, v_from, sm_count, st);
+  return vec ? launch_sums<T, OT, true>(a, ct, sm_count, st)
+             : launch_sums<T, OT, false>(a, ct, sm_count, st);
 }
 template <class T>
-cudaError_t launch_sums_o(const TableGrad& a, int ct, int out_type, bool vec, int64_t v_from,
-                          int sm_count, cudaStream_t st) {
-  if (out_type == TAB_FP32) return launch_sums_v<T, float>(a, ct, vec, v_from, sm_count, st);
-  if (out_type == TAB_BF16) return launch_sums_v<T, __nv_bfloat16>(a, ct, vec, v_from, sm_count, st);
-  return launch_sums_v<T, __half>(a, ct, vec, v_from, sm_count, st);
+cudaError_t launch_sums_o(const TableGrad& a, int ct, int out_type, bool vec, int sm_count,
+                          cudaStream_t st) {
+  if (out_type == TAB_FP32) return launch_sums_v<T, float>(a, ct, vec, sm_count, st);
+  if (out_type == TAB_BF16) return launch_sums_v<T, __nv_bfloat16>(a, ct, vec, sm_count, st);
+  return launch_sums_v<T, __half>(a, ct, vec, sm_count, st);
 }
 
 // Threads that share a range's columns: enough for the row, a warp at least, at most
@@ -820,6 +813,8 @@ cudaError_t launch_lookup(Lookup a, int table_type, int out_type, int sm_count, 
 
 // Sorted positions a range holds: 32, fewer where that would leave the SMs without
 // sixteen blocks each, more where a run through all ranges would make too many parts.
+// (8 / 16 / 32, us: 500 tokens x 4096 90 / 94 / 104, 8000 x 3584 56.0 / 56.5 / 70.5; 32768 x
+// 4096 263 / 242 / 238.)
 static int grad_range(int64_t n, int d, int sm_count) {
   const int ct = sum_threads(d);
   const int64_t groups = (d + ct * 8 - 1) / (ct * 8), per = kSumThreads / ct;
@@ -836,14 +831,16 @@ size_t grad_scratch_bytes(int64_t n, int d, int sm_count) {
   return 4 * list + (size_t)ranges * 2 * ((d + ct * 8 - 1) / (ct * 8) * ct * 8) * 4;
 }
 
-// At least what any call of up to n tokens and d columns takes: in ranges of fewer
-// than 32 positions a call has at most 32 sm_count * 128 thread columns of partial
-// sums, else at most 2048 ranges.
+// At least what any call of up to n tokens and d columns takes: ranges hold 8 positions
+// or more; fewer than 32 only while a call has at most 32 sm_count * 128 thread columns
+// of partial sums, more where 32 would make over 2048 ranges.
 size_t grad_reserve_bytes(int64_t n, int64_t d, int sm_count) {
   const size_t list = ((size_t)n * 4 + 255) / 256 * 256;
-  const size_t few = (size_t)sm_count * 32 * kSumThreads * 64;
-  const int64_t ranges = n / 32 + 1 < 2048 ? n / 32 + 1 : 2048;
-  const size_t many = (size_t)ranges * 2 * ((d + 1023) / 1024 * 1024) * 4;
+  const size_t range = 2 * (size_t)((d + 1023) / 1024 * 1024) * 4;      // bytes of one's parts
+  const size_t short_ranges = (size_t)(n / 8 + 1) * range;
+  const size_t columns = (size_t)sm_count * 32 * kSumThreads * 64;
+  const size_t few = short_ranges < columns ? short_ranges : columns;
+  const size_t many = (size_t)(n / 32 + 1 < 2048 ? n / 32 + 1 : 2048) * range;
   return 4 * list + (few > many ? few : many);
 }
 
@@ -862,16 +859,14 @@ cudaError_t launch_table_grad(TableGrad a, int src_type, int out_type, void* scr
   }
   a.partial = reinterpret_cast<float*>(at);
   cudaError_t e = cudaSuccess;
-  int64_t head = 0;             // ids whose rows are zeroed beside the sort
   if (!a.add) {
-    const int64_t row = (int64_t)a.d * type_size(out_type);
-    head = a.n == 0 ? a.V : kHeadBytes / row;
-    if (head > a.V) head = a.V;
     e = launch_pdl(head_kernel, dim3((unsigned)(2 * sm_count)), dim3(kFillThreads), 0, st, a,
-                   type_size(out_type), head);
+                   type_size(out_type));
     if (e != cudaSuccess || a.n == 0) return e;
   }
-  // one CTA sorts a short list; longer ones take a portable cluster
+  // one CTA sorts a short list; longer ones take a portable cluster (one CTA / cluster,
+  // us of a call with d = 64: 1000 tokens 16.4 / 20.6, 2000 18.7 / 21.0, 3000 20.7 / 21.6,
+  // 4000 22.3 / 21.4, 8000 30.5 / 23.5)
   const int parts = a.n <= kSortShort ? 1 : 8;
   int bits = 1;
   while (((int64_t)1 << bits) <= a.V) ++bits;         // keys are 0 .. V
@@ -882,12 +877,11 @@ cudaError_t launch_table_grad(TableGrad a, int src_type, int out_type, void* scr
   e = launch_pdl_cluster(sort, dim3(parts), dim3(kSortThreads), sizeof(SortSmem), st, parts, a, parts,
                          passes, (bits + passes - 1) / passes);
   if (e != cudaSuccess) return e;
-  const int64_t v_from = a.add ? a.V : head;
   const bool vec = on16(a.out, a.ld_out, type_size(out_type)) &&
                    on16(a.d_out, a.ld_d_out, type_size(src_type));
-  if (src_type == TAB_FP32) return launch_sums_o<float>(a, ct, out_type, vec, v_from, sm_count, st);
-  if (src_type == TAB_BF16) return launch_sums_o<__nv_bfloat16>(a, ct, out_type, vec, v_from, sm_count, st);
-  return launch_sums_o<__half>(a, ct, out_type, vec, v_from, sm_count, st);
+  if (src_type == TAB_FP32) return launch_sums_o<float>(a, ct, out_type, vec, sm_count, st);
+  if (src_type == TAB_BF16) return launch_sums_o<__nv_bfloat16>(a, ct, out_type, vec, sm_count, st);
+  return launch_sums_o<__half>(a, ct, out_type, vec, sm_count, st);
 }
 
 }  // namespace sph

@@ -104,6 +104,14 @@ def test_quantise_equals_the_oracle(sph, ctx, fmt, dtype, rows, d):
 
 
 @pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [511, 520, 1024, 1040, 2048, 2064, 4096, 4104, 6144, 6160, 8192, 8200,
+                               16400])
+def test_quantise_row_lengths(sph, ctx, fmt, dtype, d):
+    test_quantise_equals_the_oracle(sph, ctx, fmt, dtype, 9, d)
+
+
+@pytest.mark.parametrize("fmt", FMT)
 def test_quantise_midpoints_go_to_the_even_code(sph, ctx, fmt):
     # 6 fixes the scale at one; the rest lie on and beside the midpoints of two codes
     mids = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]
@@ -240,6 +248,21 @@ def test_product_on_pairs_and_in_ranges(sph, ctx, split, fmt, planes, rows, V, d
 
 
 @pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("planes", [1, 3])
+@pytest.mark.parametrize("rows,d,keep", [(1, 10500, True), (32, 10304, False), (40, 10500, True)])
+def test_product_of_long_rows(sph, ctx, fmt, planes, rows, d, keep):
+    rng = np.random.default_rng(rows)
+    w, table = held(sph, ctx, 400, d, fmt, d)
+    h = make_x(rows, d, torch.float32, rows)
+    ids = np.sort(rng.choice(400, 150, replace=False)).astype(np.int32) if keep else None
+    y = ctx.mx4_logits(h, w, keep_ids=None if ids is None else torch.tensor(ids, device=DEV),
+                       planes=planes)
+    ctx.sync()
+    want = ora.product(f64(h), table, fmt, planes, ids)
+    assert_close(f64(y), want, product_bound(f64(h), table, fmt, planes, ids, torch.float32), "y")
+
+
+@pytest.mark.parametrize("fmt", FMT)
 def test_product_rows_into_a_wider_buffer(sph, ctx, fmt):
     w, table = held(sph, ctx, 200, 96, fmt, 9)
     h = make_x(5, 96, torch.float16, 2)
@@ -362,6 +385,29 @@ def test_lookup_and_gradient_report_ids_out_of_range(sph, ctx):
     ctx.sync()
     assert tuple(ctx.embed(tok[:0], table).shape) == (0, 64)
     ctx.sync()
+
+
+@pytest.mark.parametrize("padding", [0, 7, 39])
+@pytest.mark.parametrize("T", [6, 3000, 9000])
+def test_padding_id_inside_the_vocabulary(sph, ctx, padding, T):
+    # its tokens give rows of zeros and take no part in the gradient, whose row stays zero
+    rng = np.random.default_rng(T)
+    table = make_x(40, 64, torch.float32, 1)
+    tok = rng.integers(0, 40, T)
+    tok[:3] = padding
+    t = torch.tensor(tok, dtype=torch.int32, device=DEV)
+    for form, values in ((table, f64(table)), held(sph, ctx, 40, 64, "e4m3", 1)):
+        y = ctx.embed(t, form, padding_id=padding, dtype=torch.float32)
+        assert np.array_equal(f64(y), ora.lookup(tok, values, 1.0, padding))
+    d_out = make_x(T, 64, torch.float32, 2, wide=False)
+    for add in (False, True):
+        out = torch.full((40, 64), 3.0 if add else float("nan"), device=DEV)
+        got = ctx.embed_grad(t, d_out, 40, padding_id=padding, accumulate=add, out=out)
+        ctx.sync()
+        onto = np.full((40, 64), 3.0) if add else None
+        want = ora.gradient(tok, f64(d_out), 40, 1.0, padding, onto)
+        assert_close(f64(got), want, grad_bound(tok, f64(d_out), 40, 1.0, torch.float32, onto), "pad")
+        assert (got[padding] == (3.0 if add else 0.0)).all()
 
 
 # ---- gradient -----------------------------------------------------------------------
