@@ -232,18 +232,26 @@ cudaError_t launch(const Mx4Quant& a, cudaStream_t st) {
                     dim3((unsigned)((a.rows + kRows - 1) / kRows)), dim3(kThreads), 0, st, a);
 }
 // Hidden states are few, and the product waits for them: one step a thread and as
-// many threads as a row has, up to 512.  A table's rows are many: two steps a
-// thread, a warp a row up to 1024 columns, a block of 128 threads up to 4096, of 256
-// above; each holds its row in registers up to 8192 columns.
+// many threads as a row has, up to 512 (128 / 512 threads, product and all, us: 32 x 12000
+// ids x 3840 11.7 / 10.6, 1 x 2048 x 448 6.6 / 6.9).
+// A table's rows are many, and a block's threads, waiting for each other's maxima, hide
+// less of the memory's time than as many warps with rows of their own: a warp a row up to
+// 2048 columns (16000 x 2048 fp32 27.7 us, by 128 threads 36.1; 32000 x 2048 bf16 31 and 60),
+// 128 threads above, with as many steps as hold the row in registers, up to 8192
+// columns (32000 x 5120 bf16 90.5 us, by 256 threads of two steps 134; 16000 x 4096 fp32 47.2, by a
+// warp of eight steps 52.9).  32000 x 4096 bf16 take 69.5 us, 4.8 TB/s.
 template <class T, int FMT>
 cudaError_t launch_f(const Mx4Quant& a, bool operand, cudaStream_t st) {
   if (operand) {
     if (a.scale_cols <= 128 * kCols) return launch<T, FMT, 128, 1, true>(a, st);
     return launch<T, FMT, 512, 1, true>(a, st);
   }
+  if (a.scale_cols <= 32 * 1 * kCols) return launch<T, FMT, 32, 1, false>(a, st);
   if (a.scale_cols <= 32 * 2 * kCols) return launch<T, FMT, 32, 2, false>(a, st);
+  if (a.scale_cols <= 32 * 4 * kCols) return launch<T, FMT, 32, 4, false>(a, st);
   if (a.scale_cols <= 128 * 2 * kCols) return launch<T, FMT, 128, 2, false>(a, st);
-  return launch<T, FMT, 256, 2, false>(a, st);
+  if (a.scale_cols <= 128 * 3 * kCols) return launch<T, FMT, 128, 3, false>(a, st);
+  return launch<T, FMT, 128, 4, false>(a, st);
 }
 template <class T>
 cudaError_t launch_t(const Mx4Quant& a, int fmt, bool operand, cudaStream_t st) {
