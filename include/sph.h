@@ -115,7 +115,9 @@ typedef enum sph_option {
                                SPH_ERR_TIMEOUT (default 2^34, >= 1)           */
   SPH_OPT_TC_SCHEDULE = 2,  /* tensor-core work split: 0 automatic (default),
                                1 whole vocabulary tiles per CTA, 2 contiguous
-                               k-block ranges (stream-K)                      */
+                               k-block ranges (stream-K).  sph_mx4_logits:
+                               the same of its 256-column stages; automatic
+                               takes ranges for few tiles                     */
   SPH_OPT_TC_STAGES = 3,    /* tensor-core pipeline depth: 0 automatic
                                (default), else at most this many stages (>= 2) */
   SPH_OPT_TC_BLOCK_K = 4,   /* hidden-dimension elements each pipeline stage
@@ -162,7 +164,9 @@ typedef enum sph_option {
                                either way; endpoint: >= 192);
                                1: always (SPH_ERR_UNSUPPORTED where pairs
                                cannot be scheduled);
-                               2: never.  The results are the fp32 sums of
+                               2: never.  sph_mx4_logits too, 0: for more
+                               than 96 rows in two terms or more, with kept
+                               ids in four.  The results are the fp32 sums of
                                the same products either way.               */
   SPH_OPT_SPLIT_QUANTIZE = 10, /* sph_split_step with one payload chunk: 0
                                automatic (default: in the endpoint's epilogue
@@ -625,8 +629,8 @@ sph_status sph_embed(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
                      int64_t ld_out);
 
 /* The same from a table held in 4 bits.  tokens NULL takes its first n_tokens
- * rows in order (with scale 1: the values that the table stands for, exact in
- * bf16 and fp32 unless they leave the type's range). */
+ * rows in order, whatever padding_id is (with scale 1: the values that the table
+ * stands for, exact in bf16 and fp32 unless they leave the type's range). */
 sph_status sph_embed_mx4(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
                          const sph_mx4* table, float scale,
                          int64_t padding_id, void* out, sph_tab_type out_type,

@@ -12,20 +12,26 @@
 // accumulator: 3e-6 off, in two 6e-8).
 //
 // A CTA keeps a ring of stages of 256 columns, 128 bytes of codes a row: codes by
-// TMA, W's in whole boxes where the kept ids are consecutive and four gathered
-// rows a copy elsewhere; X's scales by TMA, W's by cp.async.  Eight warps move a
+// TMA, rows of W whose kept ids are not consecutive by cp.async; X's scales by TMA,
+// W's by cp.async.  Eight warps move a
 // stage's scales from shared memory to tensor memory (in the quarter of the lanes
 // that each may write), into one of several sets of columns; one warp issues the
-// MMAs; four read the accumulator, double-buffered in tensor memory, and store.
+// MMAs; four read the accumulator and store it, while the next tile's is computed (three
+// or four terms of more rows than fit twice have one accumulator, and wait).
 // (Scales by tcgen05.cp took some 80 cycles a copy of four columns in the MMAs' own
-// queue: 1024 rows x 256000 ids x 4608 907 us.)  What bounds a stage is the MMA warp's
-// own time, so it has one barrier to wait for and one to signal, issues a stage's
-// MMAs in one piece, and takes the terms of few rows as more rows of one MMA.
+// queue: 1024 rows x 256000 ids x 4608 907 us.)
+//
+// Few rows are bound by the stream of W: 8 rows x 152064 ids x 7168 take 91.5 us,
+// 6.7 TB/s of the table's 4.5 bits an element.  Many rows are bound by the MMA warp's
+// own time a stage, some 560 cycles whatever the rows (waits, descriptors, the commit),
+// so it has one barrier to wait for and one to signal, issues a stage's MMAs in one
+// piece, and takes the terms of few rows as more rows of one MMA; and by what an SM
+// gets from the L2, some 54 bytes a cycle.  1024 rows x 256000 ids x 4608 in two terms
+// take 511 us, 9.4 PFLOP/s as issued.
 //
 // PAIR: two CTAs share a tile of 256 table rows (cta_group::2): each holds its 128
-// rows of W and half of X's codes, so that a stage costs each SM half the traffic
-// of X, in shared memory the more scarce (single CTAs moved all the bytes a cycle
-// that it has).  The even CTA issues the MMAs for both.
+// rows of W and half of X's codes, so that a stage costs each SM half the traffic of X.
+// The even CTA issues the MMAs for both.
 //
 // Work is whole tiles in turn, or, where these would leave SMs idle, equal ranges of
 // all tiles' stages: tiles cut by a range's end leave fp32 parts, and the last CTA
@@ -203,23 +209,15 @@ __device__ __forceinline__ void mma4_mx4(uint32_t d, uint32_t adesc, uint32_t bd
 #undef SPH_MMA4_HEAD
 #undef SPH_MMA4_E4M3
 #undef SPH_MMA4_E8M0
-// (bar: a shared::cluster address)
-template <bool PAIR>
+// Four rows by one copy, to a pair (bar: a shared::cluster address).
 __device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int x, int4 rows,
                                             uint32_t bar) {
-  if constexpr (PAIR)
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
-        ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
-            ptx::smem_u32(dst)),
-        "l"(map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar)
-        : "memory");
-  else
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(ptx::smem_u32(dst)),
-        "l"(map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar)
-        : "memory");
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
+      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+          ptx::smem_u32(dst)),
+      "l"(map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar)
+      : "memory");
 }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile(
@@ -316,6 +314,7 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
            const __grid_constant__ CUtensorMap map_x, const Params p) {
   constexpr int kGroups = groups_of(FMT);
   constexpr int kHalves = PAIR ? 2 : 1;         // CTAs of a unit, 128 table rows each
+  constexpr bool kPieces = GATHER && !PAIR;     // scattered rows by cp.async
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = ptx::smem_u32(smem_raw);
   const uint32_t base_addr = (raw_addr + 1023) & ~1023u;
@@ -348,7 +347,8 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      ptx::mbar_init(&full[s], 2 * kHalves);            // W and X codes of each CTA
+      // W and X codes of each CTA, scattered rows of W
+      ptx::mbar_init(&full[s], 2 * kHalves + (kPieces ? 32 : 0));
       ptx::mbar_init(&raw[s], 1);
       ptx::mbar_init(&empty[s], 1);
     }
@@ -446,17 +446,35 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
 
   if (warp == kWarpW) {
     // ---- W codes -----------------------------------------------------------
+    // Groups of 32 consecutive ids are one box.  Rows of others come as 16-byte pieces
+    // by cp.async, four rows an instruction, each piece where the 128-byte swizzle has
+    // it; on pairs, whose barriers wait for no generic writes (arrive_at), four rows a
+    // copy.  (32 rows x 12000 of 32000 ids x 3840: all ids 9.9 us, scattered ones 11.1 by
+    // cp.async, 20.6 by such copies on single CTAs.)
+    const int bytes = (g.d + 31) / 32 * 16;
     while (ok && work.next(tile, k0, k1)) {
       const int j0 = first_row(tile);
       int4 id;
       unsigned solid = 0;
+      // where rows lane / 8, lane / 8 + 4, ... begin (ids outside the table take a row of
+      // it; their scales are zeros)
+      const uint8_t* from[kPieces ? 32 : 1];
       if constexpr (GATHER) id = ids_of(tile, solid);
+      if constexpr (kPieces) {
+        if (solid != 0xFu) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int row = g.ids[min(j0 + 4 * i + (lane >> 3), (int)g.n - 1)];
+            from[i] = g.w_codes + max(0, min(row, (int)g.V - 1)) * g.ld_codes;
+          }
+        }
+      }
       for (int k = k0; k < k1; ++k) {
         if (!wait(&empty[stage], phase ^ 1, true)) { ok = false; break; }
         uint8_t* a = base + (size_t)stage * p.stage_bytes;
         const uint32_t bar = leader(&full[stage]);
         const int x = k * (kCols / 2);
-        if (lane == 0) expect(&full[stage], kABytes);
+        if (lane == 0) expect(&full[stage], kPieces ? __popc(solid) * (kABytes / 4) : kABytes);
         __syncwarp();
         auto box = [&](uint8_t* dst, int row) {
           if constexpr (PAIR) ptx::tma_load_2d_pair(dst, &map_w, x, row, bar);
@@ -465,8 +483,28 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
         if constexpr (GATHER) {
           if (solid >> (lane >> 3) & 1) {
             if ((lane & 7) == 0) box(a + lane * 512, id.x);
-          } else {
-            tma_gather4<PAIR>(a + lane * 512, &map_row, x, id, bar);
+          } else if constexpr (!kPieces) {
+            tma_gather4(a + lane * 512, &map_row, x, id, bar);
+          }
+          if constexpr (kPieces) {
+            const int piece = lane & 7, row = lane >> 3;
+            const int size = x + 16 * piece < bytes ? 16 : 0;
+            const int at = size ? x + 16 * piece : 0;
+            const uint32_t even = ptx::smem_u32(a) + row * 128 + (piece ^ row) * 16;
+            const uint32_t odd = ptx::smem_u32(a) + row * 128 + (piece ^ (row + 4)) * 16;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (solid >> q & 1) continue;
+#pragma unroll
+              for (int i = 8 * q; i < 8 * q + 8; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                 (i % 2 ? odd : even) + i * 512),
+                             "l"(from[i] + at), "r"(size)
+                             : "memory");
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(
+                             ptx::smem_u32(&full[stage]))
+                         : "memory");
           }
         } else if (lane == 0) {
           // (a pair's second half may lie past the last row: any rows of the table do,
@@ -520,6 +558,7 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       for (int i = 0; i < kM / 8; ++i) {
         const int j = j0 + 8 * i;
         id[i] = j < g.n ? (GATHER ? g.ids[j] : j) : -1;
+        if (GATHER && (uint32_t)id[i] >= (uint32_t)g.V) id[i] = -1;
       }
       for (int w = k0 / kWsStages; w * kWsStages < k1; ++w) {
         if (!wait(&ws_empty[slot], slot_phase ^ 1)) { ok = false; break; }
@@ -586,6 +625,8 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           ptx::tc_fence_before();
           if (half == 0 && !wait(&full[stage], phase)) { ok = false; break; }
+          // (what cp.async wrote is there for the MMAs' reads)
+          if constexpr (kPieces) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) arrive(&sf_full[set]);
         }
@@ -658,8 +699,8 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       const int j = first_row(tile) + in_tile;
       const bool live = j < g.n;
       float ws = 1.f, b = 0.f;
-      if (live) {
-        const int64_t id = GATHER ? g.ids[j] : j;
+      const int64_t id = !live ? -1 : GATHER ? g.ids[j] : j;
+      if (id >= 0 && id < g.V) {
         if constexpr (FMT == MX4_E4M3) ws = g.w_row[id];
         if (g.bias) b = g.bias[id];
       }
@@ -844,16 +885,19 @@ int largest(int unit, int planes, int fmt, int pair, int accs) {
 }
 // The largest tile of hidden-state rows that fits, then as many equal tiles as the rows
 // need.  Pairs where several terms make X's codes the larger part of a stage (single CTAs
-// / pairs, us: 1024 rows x 38912 ids x 4608, one term 97.5 / 107, two 158 / 140, four 372 /
-// 260; 320 x 51302 x 3584, two terms 72.3 / 70.9; 100 x 20000 x 2000, three 25.7 / 22.8;
-// 32 x 12000 x 3840, two, with the terms side by side, 12.3 / 13.4).  On pairs a tile of
+// / pairs, us, all ids: 1024 rows x 38912 ids x 4608, one term 97.5 / 107, two 158 / 140,
+// four 372 / 260; 320 x 51302 x 3584, two 72.3 / 70.9; 100 x 20000 x 2000, three 25.7 / 22.8;
+// 32 x 12000 x 3840, two, with the terms side by side, 12.3 / 13.4).  With kept ids only
+// for four terms, as pairs fetch scattered rows at half the rate (1024 x 51302 of 128256 x
+// 4608, ids in runs of 64 / scattered: two terms 209 / 213 on single CTAs, 235 / 463 on pairs;
+// three 360 / 367, 294 / 472; four 476 / 480, 342 / 480).  On pairs a tile of
 // more than 128 rows, whose scales take twice the columns, costs a third more a stage:
 // it is taken only where that saves more (the 1024 rows, two terms, in 8 tiles of 128 140
 // us, in 7 of 160 162; the 320 rows in 3 and 2 76.3 and 70.5).
 Plan plan_of(const Mx4Plan& a) {
   Plan pl{};
   pl.pair = a.pair_units > 0 &&
-            (a.pair_mode == 2 || (a.pair_mode == 1 && a.planes > 1 && a.rows > kPairRows));
+            (a.pair_mode == 2 || (a.pair_mode == 1 && a.planes > (a.gather ? 3 : 1) && a.rows > kPairRows));
   const int unit = pl.pair ? 32 : 16;         // rows a tile is a multiple of
   // two accumulators, so that a tile is stored while the next is computed; one where
   // that halves the tile's rows (three and four terms of more rows than fit so)
@@ -888,13 +932,16 @@ Plan plan_of(const Mx4Plan& a) {
   pl.sf_sets = ((int)kTmemCols - pl.sf_col) / pl.sf_cols;
   if (pl.sf_sets > kMaxSets) pl.sf_sets = kMaxSets;
   if (pl.sf_sets > pl.stages) pl.sf_sets = pl.stages;
-  // Whole tiles, or equal ranges of stages where tiles would occupy at most a third of
-  // the units: adding up the parts costs some 4 us (whole tiles / ranges, us: 1 row x 5000
-  // ids x 4096, 40 tiles, 22.0 / 15.1; 16 x 20000 x 2000, 157 tiles, 12.9 / 14.6; 32 x 12000
-  // x 3840, 94 tiles, 12.3 / 15.8).  A unit gets two stages at least.
+  // Whole tiles, or equal ranges of stages where few tiles of a long hidden dimension
+  // would leave most SMs idle: the parts' way through memory costs more than it saves
+  // below some 40 stages, and with many rows (whole tiles / ranges, us, two terms: 1 row x
+  // 5000 ids x 14336, 40 tiles of 56 stages, 22.8 / 17.3; 32 x 2000 x 14336 22.8 / 19.8;
+  // 1 x 12000 x 14336, 94 tiles, 23.6 / 22.6; 1 x 2000 x 7168 13.3 / 14.4; 32 x 5000 x 7168
+  // 13.4 / 15.5; 320 x 2000 x 3584 17.9 / 34.6).  A unit gets two stages at least.
   const int64_t most_units = pl.pair ? a.pair_units : a.sm_count;
   const int64_t stages = (int64_t)pl.tiles * pl.kt;
-  pl.ranges = a.schedule == 2 || (a.schedule == 0 && pl.kt > 4 && 3 * (int64_t)pl.tiles <= most_units);
+  pl.ranges = a.schedule == 2 || (a.schedule == 0 && pl.kt > 40 && a.rows <= 32 &&
+                                  3 * (int64_t)pl.tiles <= most_units);
   if (pl.ranges) {
     const int64_t by_two = stages / 2 > 1 ? stages / 2 : 1;
     pl.units = (int)(by_two < most_units ? by_two : most_units);
@@ -958,14 +1005,15 @@ size_t mx4_gemm_scratch_bytes(const Mx4Plan& a) {
 }
 
 // At least what any call of up to `rows` rows and d columns takes: tiles cover at
-// most 32 more rows each, and one that is not the only one has at least 32; a unit
-// leaves two parts of a tile of kMaxBn rows at most, an SM's share of them one tile's.
+// most 32 more rows each, and one that is not the only one has at least 32; an SM
+// leaves two parts of a tile at most.
 size_t mx4_gemm_reserve_bytes(int64_t rows, int64_t n, int64_t d, int sm_count) {
   const size_t r = (size_t)rows, padded = 2 * r + 64, kt = (size_t)((d + kCols - 1) / kCols);
   const size_t tiles = (size_t)((n + kM - 1) / kM + 1) * (r / 32 + 1);
   return 4 * (up256(r * ((size_t)(d + 31) / 32 * 16)) +
               up256(padded * kt * groups_of(MX4_E4M3) * 4)) +
-         up256(padded * 4) + up256(tiles * 4) + (size_t)sm_count * 2 * kMaxBn * kM * 4;
+         up256(padded * 4) + up256(tiles * 4) +
+         (size_t)sm_count * 2 * (r < kMaxBn ? (r + 31) / 32 * 32 : kMaxBn) * kM * 4;
 }
 
 cudaError_t launch_mx4_gemm(const Mx4Gemm& g, const Mx4Plan& a, void* scratch, long long spin_limit,

@@ -1394,7 +1394,7 @@ sph_status sph_mx4_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type, int6
   if (st) return st;
   const int fmt = mx4_format(W);
   const sph::Mx4Plan plan{rows, n_keep, (int)W->d, planes, fmt, ctx->sm_count, ctx->pair_units,
-                          pair_mode(ctx), ctx->tc_schedule};
+                          pair_mode(ctx), ctx->tc_schedule, keep_ids != nullptr};
   st = ensure_scratch(ctx, sph::mx4_gemm_scratch_bytes(plan));
   if (st) return st;
   sph::Mx4Gemm m{};
@@ -1457,7 +1457,7 @@ sph_status sph_embed_mx4(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
   a.table = table->codes; a.ld_table = table->ld_codes;
   a.scales = static_cast<const uint8_t*>(table->scales); a.ld_scales = table->ld_scales;
   a.row_scale = table->row_scale; a.V = table->rows; a.d = (int)table->d;
-  a.scale = scale; a.padding = padding_id; a.out = out; a.ld_out = ld_out; a.status = ctx->status;
+  a.scale = scale; a.padding = tokens ? padding_id : -1; a.out = out; a.ld_out = ld_out; a.status = ctx->status;
   return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
                          return sph::launch_lookup(a, table->format, out_type, ctx->sm_count,
                                                    ctx->stream);

@@ -357,6 +357,7 @@ struct Mx4Plan {
   int sm_count, pair_units;     // SMs, CTA pairs that fit at once
   int pair_mode;                // 0 never, 1 where it pays, 2 always
   int schedule;                 // 0 automatic, 1 whole tiles, 2 ranges of stages
+  int gather;                   // kept ids are given
 };
 size_t mx4_gemm_scratch_bytes(const Mx4Plan& a);
 size_t mx4_gemm_reserve_bytes(int64_t rows, int64_t n, int64_t d, int sm_count);
