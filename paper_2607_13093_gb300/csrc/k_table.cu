@@ -28,12 +28,45 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
   return __float2bfloat16_rn(x);
 }
 
-// A thread's eight columns of a row.  VEC: eight consecutive ones, moved in
-// 16-byte pieces (rows on 16 bytes); else `stride` apart, so that the threads of a
-// warp touch neighbouring columns whatever the row's start.
+// Eight elements of type T that start `off` bytes into the words x (less than 16): moved
+// to the words' start.
+template <class T>
+__device__ __forceinline__ void shift_words(uint32_t (&x)[2 * sizeof(T) + 4], int off) {
+  constexpr int N = 2 * (int)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < N + 3; ++i) x[i] = off & 4 ? x[i + 1] : x[i];
+#pragma unroll
+  for (int i = 0; i < N + 2; ++i) x[i] = off & 8 ? x[i + 2] : x[i];
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = __funnelshift_r(x[i], x[i + 1], off & 2 ? 16 : 0);
+  }
+}
+// Eight consecutive elements at any address, by the 16-byte words that hold them (each of
+// which holds one of the elements at least).
+template <class T>
+__device__ __forceinline__ void load_8(const T* p, float (&v)[8]) {
+  constexpr int N = (int)sizeof(T) / 2;
+  const int off = (int)((uintptr_t)p & 15);
+  const uint4* w = reinterpret_cast<const uint4*>((uintptr_t)p - off);
+  uint32_t x[4 * N + 4];
+#pragma unroll
+  for (int i = 0; i <= N; ++i) {
+    const uint4 q = i < N || off ? w[i] : make_uint4(0, 0, 0, 0);
+    x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
+  }
+  shift_words<T>(x, off);
+  const T* e = reinterpret_cast<const T*>(x);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
+}
+
+// A thread's eight columns of a row, col .. col + 7 (those in 0 .. d - 1; zeros for the
+// others).  VEC: rows and col are on 16 bytes.
 template <class T, bool VEC>
-__device__ __forceinline__ void load_cols(const T* row, int col, int stride, int d, float (&v)[8]) {
-  if (VEC && col + 8 <= d) {
+__device__ __forceinline__ void load_cols(const T* row, int col, int d, float (&v)[8]) {
+  const bool all = (VEC || col >= 0) && col + 8 <= d;
+  if (VEC && all) {
     uint4 w[sizeof(T) / 2];
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i)
@@ -41,15 +74,18 @@ __device__ __forceinline__ void load_cols(const T* row, int col, int stride, int
     const T* e = reinterpret_cast<const T*>(w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
+  } else if (all) {
+    load_8(row + col, v);
   } else {
-    const int s = VEC ? 1 : stride;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = col + j * s < d ? to_f32(row[col + j * s]) : 0.f;
+    for (int j = 0; j < 8; ++j)
+      v[j] = col + j >= 0 && col + j < d ? to_f32(row[col + j]) : 0.f;
   }
 }
-template <class T, bool VEC>
-__device__ __forceinline__ void store_cols(T* row, int col, int stride, int d, const float (&v)[8]) {
-  if (VEC && col + 8 <= d) {
+// ON16: row + col is on 16 bytes.
+template <class T, bool ON16>
+__device__ __forceinline__ void store_cols(T* row, int col, int d, const float (&v)[8]) {
+  if (ON16 && col >= 0 && col + 8 <= d) {
     uint4 w[sizeof(T) / 2];
     T* e = reinterpret_cast<T*>(w);
 #pragma unroll
@@ -57,10 +93,9 @@ __device__ __forceinline__ void store_cols(T* row, int col, int stride, int d, c
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + col)[i] = w[i];
   } else {
-    const int s = VEC ? 1 : stride;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (col + j * s < d) row[col + j * s] = from_f32<T>(v[j]);
+      if (col + j >= 0 && col + j < d) row[col + j] = from_f32<T>(v[j]);
   }
 }
 
@@ -73,11 +108,12 @@ constexpr int kLookSpan = kLookThreads * 8;    // columns of a block
 struct Mx4Row;     // tag of a table held in 4 bits (FMT says which)
 
 // A thread's eight columns of a table row as they lie in memory, and their values.
+// VEC: rows of table and output, and so col, are on 16 bytes.
 template <class TT, int FMT, bool VEC>
 struct Piece {           // dense rows
   float v[8];
   __device__ __forceinline__ void load(const Lookup& a, int64_t id, int col) {
-    load_cols<TT, VEC>(static_cast<const TT*>(a.table) + id * a.ld_table, col, kLookThreads, a.d, v);
+    load_cols<TT, VEC>(static_cast<const TT*>(a.table) + id * a.ld_table, col, a.d, v);
   }
   __device__ __forceinline__ void values(float, float (&x)[8]) const {
 #pragma unroll
@@ -85,7 +121,7 @@ struct Piece {           // dense rows
   }
 };
 template <int FMT>
-struct Piece<Mx4Row, FMT, true> {      // eight consecutive columns in 4 bits
+struct Piece<Mx4Row, FMT, true> {      // in 4 bits
   uint32_t codes;
   uint8_t scale;
   __device__ __forceinline__ void load(const Lookup& a, int64_t id, int col) {
@@ -101,27 +137,27 @@ struct Piece<Mx4Row, FMT, true> {      // eight consecutive columns in 4 bits
   }
 };
 template <int FMT>
-struct Piece<Mx4Row, FMT, false> {     // columns kLookThreads apart
-  uint8_t codes[8], scale[8];
-  int odd;
+struct Piece<Mx4Row, FMT, false> {     // columns of two words, and of two blocks
+  uint32_t codes;
+  uint8_t scale, next;
+  int left;                            // columns of the first block
   __device__ __forceinline__ void load(const Lookup& a, int64_t id, int col) {
-    const uint8_t* c = static_cast<const uint8_t*>(a.table) + id * a.ld_table;
+    constexpr int B = Mx4<FMT>::kBlock;
+    const uint32_t* c = reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.table) +
+                                                          id * a.ld_table);
     const uint8_t* s = a.scales + id * a.ld_scales;
-    odd = col & 1;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int at = min(col + j * kLookThreads, a.d - 1);
-      codes[j] = c[at / 2];
-      scale[j] = s[at / Mx4<FMT>::kBlock];
-    }
+    const int from = max(col, 0), i = from / 8;
+    const uint32_t hi = from % 8 && 8 * i + 8 < a.d ? c[i + 1] : 0u;
+    codes = __funnelshift_r(c[i], hi, from % 8 * 4) << 4 * (from - col);
+    scale = s[from / B];
+    next = s[min(col + 7, a.d - 1) / B];
+    left = B - (col & (B - 1));        // (col < 0: no more than -col, so all are the next's)
   }
   __device__ __forceinline__ void values(float row, float (&x)[8]) const {
-    uint32_t w = 0;
+    e2m1x8_to_float(codes, x);
+    const float s = mx4_scale_value<FMT>(scale) * row, t = mx4_scale_value<FMT>(next) * row;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w |= (uint32_t)(codes[j] >> 4 * odd & 15) << 4 * j;
-    e2m1x8_to_float(w, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= mx4_scale_value<FMT>(scale[j]) * row;
+    for (int j = 0; j < 8; ++j) x[j] *= j < left ? s : t;
   }
 };
 
@@ -132,13 +168,17 @@ __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const Lookup a) {
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int64_t t = blockIdx.x / a.blocks;
-  const int first = (int)(blockIdx.x % a.blocks) * a.turns * kLookSpan +
-                    (VEC ? (int)threadIdx.x * 8 : (int)threadIdx.x);
+  const int span = (int)(blockIdx.x % a.blocks) * a.turns;
   const int64_t id = a.tokens ? a.tokens[t] : t;
   const bool there = id >= 0 && id < a.V && id != a.padding;
-  if (!there && id != a.padding && first == 0) atomicOr(a.status, ERR_BAD_INDEX);
+  if (!there && id != a.padding && span == 0 && threadIdx.x == 0) atomicOr(a.status, ERR_BAD_INDEX);
   const float row = FMT == MX4_E4M3 && there ? a.row_scale[id] : 1.f;
   OT* out = static_cast<OT*>(a.out) + t * a.ld_out;
+  // the first piece ends at the output row's first 16-byte boundary, so that the others
+  // are stored in 16-byte words (element by element, us: 16384 x 5119 bf16 171, from e4m3
+  // 121; 32000 x 4095 from e4m3 176)
+  const int head = VEC ? 0 : (int)(-(intptr_t)out & 15) / (int)sizeof(OT);
+  const int first = span * kLookSpan + (int)threadIdx.x * 8 + (head ? head - 8 : 0);
   for (int n = 0; n < a.turns; n += U) {
     Piece<TT, FMT, VEC> piece[U];
 #pragma unroll
@@ -158,7 +198,7 @@ __global__ void __launch_bounds__(kLookThreads) lookup_kernel(const Lookup a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= a.scale;
       }
-      store_cols<OT, VEC>(out, col, kLookThreads, a.d, v);
+      store_cols<OT, true>(out, col, a.d, v);
     }
   }
 }
@@ -168,7 +208,7 @@ cudaError_t launch_lookup_v(Lookup a, int sm_count, cudaStream_t st) {
   // One block a token once that gives every SM two, else a block for each span
   // (a block a token / a span, us, into bf16: 32 tokens x 5120 from e4m3 2.8 / 2.4, 500
   // 3.5 / 4.1, 1200 4.5 / 7.4; 32 x 4096 from bf16 3.1 / 2.5, 500 3.7 / 3.6, 1200 4.6 / 6.2).
-  const int spans = (a.d + kLookSpan - 1) / kLookSpan;
+  const int spans = (a.d + (VEC ? 0 : 7) + kLookSpan - 1) / kLookSpan;
   a.turns = a.n >= (int64_t)sm_count * 2 ? spans : 1;
   a.blocks = (spans + a.turns - 1) / a.turns;
   const dim3 grid((unsigned)(a.n * a.blocks));
@@ -493,19 +533,60 @@ constexpr int kSumThreads = 128, kJoinThreads = 512;
 constexpr int kSumBytes = 256;      // shared memory of a thread: rows requested ahead
 constexpr int kShortRun = 16;       // (at most 32) positions of a run that one range takes whole
 
-// Columns of thread `u` of `ct` in column group g.
-template <bool VEC>
-__device__ __forceinline__ int sum_col(int g, int u, int ct) {
-  return g * ct * 8 + (VEC ? u * 8 : u);
+// First column of thread `u` of `ct` in column group g.
+__device__ __forceinline__ int sum_col(int g, int u, int ct) { return (g * ct + u) * 8; }
+
+// A row of any address, each lane of a warp having eight columns of it, one lane's after
+// the other's: lanes store the 16-byte words in which their columns begin, with the
+// neighbour's last ones; the first and the last lane what is left, by elements.  For
+// whole warps.
+template <class OT>
+__device__ __forceinline__ void store_shifted(OT* row, int col, int d, const float (&v)[8]) {
+  constexpr int N = 2 * (int)sizeof(OT);
+  const int lane = threadIdx.x & 31, off = (int)((uintptr_t)(row + col) & 15);
+  const int extra = off / (int)sizeof(OT);       // columns of the neighbour
+  OT own[8];
+  uint32_t x[N + 4];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) own[j] = from_f32<OT>(v[j]);
+  memcpy(x + 4, own, sizeof(own));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = __shfl_up_sync(0xFFFFFFFFu, x[N + i], 1);
+  if (off == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = x[i + 4];
+  } else {
+    shift_words<OT>(x, 16 - off);
+  }
+  const int first = col - extra;
+  if ((lane > 0 || extra == 0) && first + 8 <= d) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      reinterpret_cast<uint4*>(row + first)[i] =
+          make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+  } else {
+    const OT* e = reinterpret_cast<const OT*>(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if ((lane > 0 || j >= extra) && first + j < d) row[first + j] = e[j];
+  }
+  if (lane == 31) {
+#pragma unroll
+    for (int j = 1; j < 8; ++j)
+      if (j >= 8 - extra && col + j < d) row[col + j] = own[j];
+  }
 }
 
+// (for whole warps)
 template <class OT, bool VEC>
-__device__ __forceinline__ void write_row(const TableGrad& a, int32_t id, int col, int ct,
+__device__ __forceinline__ void write_row(const TableGrad& a, int32_t id, int col,
                                           const float (&sum)[8], const float (&onto)[8]) {
   float v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = onto[j] + a.scale * sum[j];
-  store_cols<OT, VEC>(static_cast<OT*>(a.out) + (int64_t)id * a.ld_out, col, ct, a.d, v);
+  OT* row = static_cast<OT*>(a.out) + (int64_t)id * a.ld_out;
+  if constexpr (!VEC) store_shifted<OT>(row, col, a.d, v);
+  else if (col < a.d) store_cols<OT, true>(row, col, a.d, v);
 }
 
 // ct threads (whole warps) a range of a.range sorted positions and 8 ct columns, 128 /
@@ -513,19 +594,22 @@ __device__ __forceinline__ void write_row(const TableGrad& a, int32_t id, int co
 // the range that it begins in and written out; of a longer one each range sums its
 // own part, into slot 2 r of the partial sums where the run began earlier, into
 // slot 2 r + 1 where it begins in the range and goes on (written out where it does
-// neither).  Lanes hold the ids and positions of 32 sorted places each; a thread's
-// columns of the next rows are on their way to its own piece of shared memory
-// while it adds, and nothing is shared between threads.  ADD: so is what the table
-// holds for a run, requested with its first row (read at the run's end, it made each
-// run wait for memory: 8000 rows x 3584 41 us).  (With rows in registers the code for a
+// neither).  Lanes hold the ids and positions of 32 sorted places each; the words that
+// hold a thread's columns of the next rows are on their way to its own piece of shared
+// memory while it adds, and nothing is shared between threads.  ADD: so is what the
+// table holds for a run, requested with its first row (read at the run's end, it made
+// each run wait for memory: 8000 rows x 3584 41 us).  Rows off 16 bytes are shifted into
+// place as they are taken, and back as they are stored (element by element: 32768 x 4095
+// bf16, the whole call, 541 us; so 289, and 229 for 4096).  (With rows in registers the code for a
 // run's end stood once for each of them: 32768 rows x 4096 bf16 159 us.)
 template <class T, class OT, bool VEC, bool ADD>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int ct) {
-  // pieces of 16 bytes a slot: the row's, then the table's (not VEC: eight floats)
-  constexpr int kPieces = VEC ? (int)sizeof(T) / 2 : 2;
-  constexpr int kOnto = VEC && ADD ? (int)sizeof(OT) / 2 : 0;
+  // 16-byte words a slot: the row's, then the table's (not VEC: those that hold the
+  // thread's columns)
+  constexpr int kPieces = (int)sizeof(T) / 2 + !VEC;
+  constexpr int kOnto = ADD ? (int)sizeof(OT) / 2 + !VEC : 0;
   constexpr int kFit = kSumBytes / 16 / (kPieces + kOnto);
-  constexpr int kAhead = !VEC ? 8 : kFit >= 16 ? 16 : kFit >= 8 ? 8 : 4;
+  constexpr int kAhead = kFit >= 16 ? 16 : kFit >= 8 ? 8 : 4;
   __shared__ uint4 s_rows[kAhead * (kPieces + kOnto)][kSumThreads];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
@@ -533,7 +617,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
   const int group = (int)(blockIdx.x % a.groups);
   const int64_t r = (int64_t)(blockIdx.x / a.groups) * (kSumThreads / ct) + threadIdx.x / ct;
   if (r * a.range >= a.n) return;
-  const int col = sum_col<VEC>(group, u, ct);
+  const int col = sum_col(group, u, ct);
   const bool active = col < a.d;
   const int i0 = (int)(r * a.range), i1 = min(a.n, i0 + a.range);
   const int32_t* keys = a.keys[0];
@@ -579,10 +663,9 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
   int32_t next_key = window(keys, begin + 32), next_at = window(pos, begin + 32);
   int32_t cur = __shfl_sync(0xFFFFFFFFu, key, 0);
   auto flush = [&](bool right) {
-    if (!active) return;
     if (!open_left && !right) {
-      write_row<OT, VEC>(a, cur, col, ct, acc, onto);
-    } else {
+      write_row<OT, VEC>(a, cur, col, acc, onto);
+    } else if (active) {
       float* p = a.partial + (2 * r + (open_left ? 0 : 1)) * a.ld_partial + group * ct * 8 + u * 8;
       reinterpret_cast<float4*>(p)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
       reinterpret_cast<float4*>(p)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
@@ -605,16 +688,43 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
     return static_cast<const T*>(a.d_out) + (int64_t)t * a.ld_d_out;
   };
   const bool inside = col + 8 <= a.d;
-  auto copy16 = [&](uint4* dst, const void* row, int q, int size) {
+  // word q of those that hold the thread's columns, from p on, of `size` bytes each
+  auto copy16 = [&](uint4* dst, const void* p, int q, int size) {
+    const int off = VEC ? 0 : (int)((uintptr_t)p & 15);
     // columns past the row's last are zeros, and not read
-    const int bytes = inside ? 16 : min(16, max(0, (a.d - col) * size - 16 * q));
-    if (active)
+    const int left = (inside ? 8 : a.d - col) * size + off - 16 * q;
+    const int bytes = VEC && inside ? 16 : min(16, max(0, left));
+    const void* src = static_cast<const uint8_t*>(p) - off + (bytes > 0 ? 16 * q : 0);
+    if (!active) return;
+    if (VEC && size == 2)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)),
-                   "l"(static_cast<const uint4*>(row) + (bytes > 0 ? q : 0)), "r"(bytes)
+                   "l"(src), "r"(bytes)
+                   : "memory");
+    else       // (what two lanes, or two words of a lane, share is read from the L2 once)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(dst)),
+                   "l"(src), "r"(bytes)
                    : "memory");
   };
+  // the columns out of the words of a slot, which came from p on
+  auto take = [&](auto type, const uint4* slot_words, const void* p, float (&v)[8]) {
+    using E = decltype(type);
+    constexpr int N = (int)sizeof(E) / 2;
+    uint32_t x[4 * N + 4];
+#pragma unroll
+    for (int h = 0; h < N + !VEC; ++h) {
+      const uint4 w = slot_words[h * kSumThreads];
+      x[4 * h] = w.x; x[4 * h + 1] = w.y; x[4 * h + 2] = w.z; x[4 * h + 3] = w.w;
+    }
+    if constexpr (!VEC) shift_words<E>(x, (int)((uintptr_t)p & 15));
+    const E* e = reinterpret_cast<const E*>(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
+  };
+  auto table_row = [&](int32_t k) {
+    return static_cast<const OT*>(a.out) + (int64_t)k * a.ld_out + col;
+  };
   int32_t asked = -1;                       // the id of the last place requested
-  auto request = [&](int w0, int i) {       // (VEC) place i, of the window from w0
+  auto request = [&](int w0, int i) {       // place i, of the window from w0
     if (i < end) {
       const int slot = (i - begin) % kAhead * (kPieces + kOnto);
       const T* row = row_of(i - w0) + col;
@@ -623,7 +733,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
       if constexpr (ADD) {
         const int32_t k = __shfl_sync(0xFFFFFFFFu, i - w0 < 32 ? key : next_key, (i - w0) & 31);
         if (k != asked) {
-          const OT* t = static_cast<const OT*>(a.out) + (int64_t)k * a.ld_out + col;
+          const OT* t = table_row(k);
 #pragma unroll
           for (int q = 0; q < kOnto; ++q)
             copy16(&s_rows[slot + kPieces + q][threadIdx.x], t, q, sizeof(OT));
@@ -633,66 +743,22 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if constexpr (VEC) {
-    for (int i = 0; i < kAhead - 1; ++i) request(begin, begin + i);
-  }
+  for (int i = 0; i < kAhead - 1; ++i) request(begin, begin + i);
   int32_t last = -1;
   for (int w0 = begin; w0 < end; w0 += 32) {
     const int count = min(32, end - w0);
-    if constexpr (VEC) {
-      for (int q = 0; q < count; ++q) {
-        request(w0, w0 + q + kAhead - 1);
-        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-        uint4 w[kPieces];
-        const int slot = (w0 + q - begin) % kAhead * (kPieces + kOnto);
-#pragma unroll
-        for (int h = 0; h < kPieces; ++h) w[h] = s_rows[slot + h][threadIdx.x];
-        const T* e = reinterpret_cast<const T*>(w);
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = to_f32(e[j]);
-        const int32_t k = __shfl_sync(0xFFFFFFFFu, key, q);
-        add(k, x);
-        if constexpr (ADD) {
-          if (w0 + q == begin || k != last) {      // (a run's first row: what it is added to)
-            uint4 t[kOnto];
-#pragma unroll
-            for (int h = 0; h < kOnto; ++h) t[h] = s_rows[slot + kPieces + h][threadIdx.x];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) onto[j] = to_f32(reinterpret_cast<const OT*>(t)[j]);
-          }
-          last = k;
-        }
-      }
-    } else {
-      for (int b = 0; b < count; b += kAhead) {
-        const int m = min(kAhead, count - b);
-        for (int h = 0; h < m; h += 4) {
-          float x[4][8];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const T* row = row_of(min(b + h + q, 31));
-            if (h + q < m) load_cols<T, false>(row, col, ct, a.d, x[q]);
-          }
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (h + q < m) {
-              s_rows[2 * (h + q)][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][0]);
-              s_rows[2 * (h + q) + 1][threadIdx.x] = *reinterpret_cast<const uint4*>(&x[q][4]);
-            }
-        }
-        for (int q = 0; q < m; ++q) {
-          const uint4 lo = s_rows[2 * q][threadIdx.x], hi = s_rows[2 * q + 1][threadIdx.x];
-          const float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z),
-                              __uint_as_float(lo.w), __uint_as_float(hi.x), __uint_as_float(hi.y),
-                              __uint_as_float(hi.z), __uint_as_float(hi.w)};
-          const int32_t k = __shfl_sync(0xFFFFFFFFu, key, b + q);
-          add(k, x);
-          if (ADD && k != last && active)
-            load_cols<OT, false>(static_cast<const OT*>(a.out) + (int64_t)k * a.ld_out, col, ct, a.d,
-                                 onto);
-          last = k;
-        }
+    for (int q = 0; q < count; ++q) {
+      request(w0, w0 + q + kAhead - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+      const uint4* slot = &s_rows[(w0 + q - begin) % kAhead * (kPieces + kOnto)][threadIdx.x];
+      float x[8];
+      take(T(), slot, VEC ? nullptr : row_of(q) + col, x);
+      const int32_t k = __shfl_sync(0xFFFFFFFFu, key, q);
+      add(k, x);
+      if constexpr (ADD) {
+        // a run's first row: what it is added to
+        if (w0 + q == begin || k != last) take(OT(), slot + kPieces * kSumThreads, table_row(k), onto);
+        last = k;
       }
     }
     key = next_key;
@@ -728,7 +794,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const TableGrad a, i
       if (c < kJoinThreads) break;
     }
     const int u = threadIdx.x % ct, share = threadIdx.x / ct, shares = kJoinThreads / ct;
-    const int col = sum_col<VEC>(group, u, ct);
+    const int col = sum_col(group, u, ct);
     float sum[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] = 0.f;
@@ -746,16 +812,16 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const TableGrad a, i
 #pragma unroll
     for (int j = 0; j < 8; ++j) s_sum[j * kJoinThreads + threadIdx.x] = sum[j];
     __syncthreads();
-    if (share == 0 && col < a.d) {
+    if (share == 0) {
       for (int h = 1; h < shares; ++h)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += s_sum[j * kJoinThreads + h * ct + u];
       float onto[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) onto[j] = 0.f;
-      if (a.add)
-        load_cols<OT, VEC>(static_cast<const OT*>(a.out) + (int64_t)id * a.ld_out, col, ct, a.d, onto);
-      write_row<OT, VEC>(a, id, col, ct, sum, onto);
+      if (a.add && col < a.d)
+        load_cols<OT, VEC>(static_cast<const OT*>(a.out) + (int64_t)id * a.ld_out, col, a.d, onto);
+      write_row<OT, VEC>(a, id, col, sum, onto);
     }
     __syncthreads();
   }

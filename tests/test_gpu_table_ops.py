@@ -410,6 +410,25 @@ def test_padding_id_inside_the_vocabulary(sph, ctx, padding, T):
         assert (got[padding] == (3.0 if add else 0.0)).all()
 
 
+@pytest.mark.parametrize("off", range(8))
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [5, 8, 23, 250, 1031])
+def test_lookup_at_every_alignment(sph, ctx, out, off, d):
+    # the other row stride is odd: the rows of a call have every alignment of their own too
+    T, V, W = 40, 17, 1047
+    tok = np.random.default_rng(off).integers(0, V, T)
+    t = torch.tensor(tok, dtype=torch.int32, device=DEV)
+    src = torch.full((V, W + 2), float("nan"), dtype=torch.bfloat16, device=DEV)
+    src[:, 7 - off:7 - off + d] = make_x(V, d, torch.bfloat16, d)
+    for table, values in ((src[:, 7 - off:7 - off + d], f64(src[:, 7 - off:7 - off + d])),
+                          held(sph, ctx, V, d, "e4m3", d), held(sph, ctx, V, d, "e8m0", d)):
+        buf = torch.full((T, W), 7.0, dtype=out, device=DEV)
+        ctx.embed(t, table, out=buf[:, off:off + d])
+        ctx.sync()
+        assert np.array_equal(f64(buf[:, off:off + d]), ora.lookup(tok, values, 1.0))
+        assert (buf[:, :off] == 7).all() and (buf[:, off + d:] == 7).all()
+
+
 # ---- gradient -----------------------------------------------------------------------
 def grad_bound(tok, d_out, V, scale, out, onto=None):
     """Bound of an fp32 sum in any order, and the roundings after it."""
@@ -544,6 +563,28 @@ def test_gradient_into_unaligned_slices(sph, ctx):
     assert_close(f64(buf[:, 1:196]), want,
                  grad_bound(tok.cpu().numpy(), f64(src), 30, 1.0, torch.bfloat16), "slice")
     assert (buf[:, 0] == 5).all() and (buf[:, 196:] == 5).all()
+
+
+@pytest.mark.parametrize("off", range(8))
+@pytest.mark.parametrize("src,out", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16),
+                                     (torch.float16, torch.float32), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("d", [5, 8, 250, 1031])
+def test_gradient_at_every_alignment(sph, ctx, src, out, add, off, d):
+    T, V, W = 90, 23, 1047
+    tok = np.random.default_rng(off).integers(0, V // 2, T)       # (long and short runs)
+    tok[-30:] = V - 1
+    t = torch.tensor(tok, dtype=torch.int32, device=DEV)
+    rows = torch.full((T, W + 2), float("nan"), dtype=src, device=DEV)
+    g = rows[:, 7 - off:7 - off + d]
+    g.copy_(make_x(T, d, src, d, wide=False))
+    buf = torch.full((V, W), 7.0, dtype=out, device=DEV)
+    ctx.embed_grad(t, g, V, accumulate=add, out=buf[:, off:off + d])
+    ctx.sync()
+    onto = np.full((V, d), 7.0) if add else None
+    want = ora.gradient(tok, f64(g), V, 1.0, -1, onto)
+    assert_close(f64(buf[:, off:off + d]), want, grad_bound(tok, f64(g), V, 1.0, out, onto), "g")
+    assert (buf[:, :off] == 7).all() and (buf[:, off + d:] == 7).all()
 
 
 def test_gradient_against_differences(sph, ctx):
