@@ -8,7 +8,7 @@
 // read, 16 consecutive columns a thread and step, while the row's and the blocks'
 // maxima are made; rows too long for the registers are read twice.  What a
 // block's scale costs is shared by its 16 columns (with 8 columns a thread,
-// 32000 x 4096 bf16 rows took 125 us).
+// 32000 x 4096 bf16 rows took 125 us, the readback included; so 113).
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -40,47 +40,37 @@ template <> __device__ __forceinline__ float element<__nv_bfloat16>(const Raw<__
   return __uint_as_float(j % 2 ? w & 0xFFFF0000u : w << 16);
 }
 
-// Columns col .. col + 15 of each lane's row part (a warp's lanes hold 512
-// consecutive columns of one row); zeros past column d.  aligned: the row starts on
-// 16 bytes.  Other rows go through the warp's piece of shared memory, so that
-// neighbouring lanes read neighbouring columns.  Coherent loads: the caller's
-// kernel may have written x just before.
+// Columns col .. col + 15 of a row, zeros past column d.  aligned: the row starts on 16
+// bytes.  Other rows are read by the 16-byte words that hold the columns (each of which
+// holds one at least) and shifted (32000 x 4095 bf16 75 us; column by column through
+// shared memory 93).  Coherent loads: the caller's kernel may have
+// written x just before.
 template <class T>
-__device__ __forceinline__ void load_raw(const T* row, int col, int d, bool aligned, T* stage,
-                                         int lane, Raw<T>& r) {
-  if (aligned && col + kCols <= d) {
+__device__ __forceinline__ void load_raw(const T* row, int col, int d, bool aligned, Raw<T>& r) {
+  constexpr int N = (int)sizeof(T);             // 16-byte words of the columns
+  if (col + kCols > d) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = reinterpret_cast<const uint4*>(row + col)[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = make_uint4(0, 0, 0, 0);
-    if (aligned) {
-      T* e = reinterpret_cast<T*>(r.w);
-#pragma unroll
-      for (int j = 0; j < kCols; ++j)
-        if (col + j < d) e[j] = row[col + j];
-    }
-  }
-  if (!aligned) {
-    // lane l's 16 columns start at 18 l (17 l for fp32): no two lanes in one bank
-    constexpr int kPitch = kCols + (sizeof(T) == 4 ? 1 : 2);
-    const int first = col - lane * kCols;
-    T v[kCols];
-#pragma unroll
-    for (int j = 0; j < kCols; ++j) {
-      const int c = j * 32 + lane;
-      v[j] = first + c < d ? row[first + c] : T(0.f);
-    }
-#pragma unroll
-    for (int j = 0; j < kCols; ++j) {
-      const int c = j * 32 + lane;
-      stage[c / kCols * kPitch + c % kCols] = v[j];
-    }
-    __syncwarp();
+    for (int i = 0; i < N; ++i) r.w[i] = make_uint4(0, 0, 0, 0);
     T* e = reinterpret_cast<T*>(r.w);
 #pragma unroll
-    for (int j = 0; j < kCols; ++j) e[j] = stage[lane * kPitch + j];
-    __syncwarp();
+    for (int j = 0; j < kCols; ++j)
+      if (col + j < d) e[j] = row[col + j];
+  } else if (aligned) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.w[i] = reinterpret_cast<const uint4*>(row + col)[i];
+  } else {
+    const int off = (int)((uintptr_t)(row + col) & 15);
+    const uint4* w = reinterpret_cast<const uint4*>((uintptr_t)(row + col) - off);
+    uint32_t x[4 * N + 4];
+#pragma unroll
+    for (int i = 0; i <= N; ++i) {
+      const uint4 q = i < N || off ? w[i] : make_uint4(0, 0, 0, 0);
+      x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
+    }
+    shift_words<4 * N, N>(x, off);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      r.w[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
   }
 }
 
@@ -120,7 +110,6 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) quant_kernel(const Mx4Q
   constexpr int kThreads = TPR < 128 ? 128 : TPR;
   constexpr int kRows = kThreads / TPR;                // rows of a block
   constexpr int kSpan = TPR * U;                       // steps a turn
-  __shared__ T s_stage[kThreads / 32][32 * (kCols + 2)];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   if constexpr (OPERAND) {
@@ -132,7 +121,6 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) quant_kernel(const Mx4Q
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
   if (row >= a.rows) return;                           // (whole warps; TPR >= 128: whole blocks)
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  T* stage = s_stage[threadIdx.x / 32];
   const bool aligned = a.aligned != 0;
   const int turns = (a.scale_cols / kCols + kSpan - 1) / kSpan;
   Raw<T> raw[U];
@@ -140,7 +128,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) quant_kernel(const Mx4Q
   auto load = [&](int turn) {
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      load_raw<T>(x, (turn * kSpan + i * TPR + t) * kCols, a.d, aligned, stage, lane, raw[i]);
+      load_raw<T>(x, (turn * kSpan + i * TPR + t) * kCols, a.d, aligned, raw[i]);
 #pragma unroll
     for (int i = 0; i < U; ++i) amax[i] = block_amax<FMT>(raw[i]);
   };
@@ -232,14 +220,14 @@ cudaError_t launch(const Mx4Quant& a, cudaStream_t st) {
                     dim3((unsigned)((a.rows + kRows - 1) / kRows)), dim3(kThreads), 0, st, a);
 }
 // Hidden states are few, and the product waits for them: one step a thread and as
-// many threads as a row has, up to 512 (128 / 512 threads, product and all, us: 32 x 12000
-// ids x 3840 11.7 / 10.6, 1 x 2048 x 448 6.6 / 6.9).
+// many threads as a row has, up to 512 (128 / 512 threads, the product and all, us: 32 x
+// 12000 ids x 3840 11.3 / 10.2, 320 x 12000 x 3584 28.6 / 25.7, 1 x 2048 x 448 6.5 / 6.8).
 // A table's rows are many, and a block's threads, waiting for each other's maxima, hide
 // less of the memory's time than as many warps with rows of their own: a warp a row up to
-// 2048 columns (16000 x 2048 fp32 27.7 us, by 128 threads 36.1; 32000 x 2048 bf16 31 and 60),
-// 128 threads above, with as many steps as hold the row in registers, up to 8192
-// columns (32000 x 5120 bf16 90.5 us, by 256 threads of two steps 134; 16000 x 4096 fp32 47.2, by a
-// warp of eight steps 52.9).  32000 x 4096 bf16 take 69.5 us, 4.8 TB/s.
+// 2048 columns (32000 x 2048 bf16 28.9 us, by 128 threads 46.7), 128 threads above, with
+// as many steps as hold the row in registers, up to 8192 columns (32000 x 5120 bf16
+// three steps 73, four 81, 256 threads of two 101; 16000 x 4096 fp32 44.7, by a warp of eight
+// steps 50.0).  32000 x 4096 bf16 take 59.5 us, 5.6 TB/s.
 template <class T, int FMT>
 cudaError_t launch_f(const Mx4Quant& a, bool operand, cudaStream_t st) {
   if (operand) {

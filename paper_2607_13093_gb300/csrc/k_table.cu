@@ -28,34 +28,20 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
   return __float2bfloat16_rn(x);
 }
 
-// Eight elements of type T that start `off` bytes into the words x (less than 16): moved
-// to the words' start.
-template <class T>
-__device__ __forceinline__ void shift_words(uint32_t (&x)[2 * sizeof(T) + 4], int off) {
-  constexpr int N = 2 * (int)sizeof(T);
-#pragma unroll
-  for (int i = 0; i < N + 3; ++i) x[i] = off & 4 ? x[i + 1] : x[i];
-#pragma unroll
-  for (int i = 0; i < N + 2; ++i) x[i] = off & 8 ? x[i + 2] : x[i];
-  if constexpr (sizeof(T) == 2) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = __funnelshift_r(x[i], x[i + 1], off & 2 ? 16 : 0);
-  }
-}
 // Eight consecutive elements at any address, by the 16-byte words that hold them (each of
 // which holds one of the elements at least).
 template <class T>
 __device__ __forceinline__ void load_8(const T* p, float (&v)[8]) {
-  constexpr int N = (int)sizeof(T) / 2;
+  constexpr int N = 2 * (int)sizeof(T);         // words
   const int off = (int)((uintptr_t)p & 15);
   const uint4* w = reinterpret_cast<const uint4*>((uintptr_t)p - off);
-  uint32_t x[4 * N + 4];
+  uint32_t x[N + 4];
 #pragma unroll
-  for (int i = 0; i <= N; ++i) {
-    const uint4 q = i < N || off ? w[i] : make_uint4(0, 0, 0, 0);
+  for (int i = 0; i <= N / 4; ++i) {
+    const uint4 q = i < N / 4 || off ? w[i] : make_uint4(0, 0, 0, 0);
     x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
   }
-  shift_words<T>(x, off);
+  shift_words<N, sizeof(T)>(x, off);
   const T* e = reinterpret_cast<const T*>(x);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
@@ -556,7 +542,7 @@ __device__ __forceinline__ void store_shifted(OT* row, int col, int d, const flo
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = x[i + 4];
   } else {
-    shift_words<OT>(x, 16 - off);
+    shift_words<N, sizeof(OT)>(x, 16 - off);
   }
   const int first = col - extra;
   if ((lane > 0 || extra == 0) && first + 8 <= d) {
@@ -715,7 +701,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const TableGrad a, int
       const uint4 w = slot_words[h * kSumThreads];
       x[4 * h] = w.x; x[4 * h + 1] = w.y; x[4 * h + 2] = w.z; x[4 * h + 3] = w.w;
     }
-    if constexpr (!VEC) shift_words<E>(x, (int)((uintptr_t)p & 15));
+    if constexpr (!VEC) shift_words<4 * N, sizeof(E)>(x, (int)((uintptr_t)p & 15));
     const E* e = reinterpret_cast<const E*>(x);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);

@@ -120,4 +120,18 @@ __device__ __forceinline__ void mx4_codes(const float (&x)[N], float step, uint3
   }
 }
 
+// N words of elements of SIZE bytes that start `off` bytes into x (less than 16): moved to
+// x's start.
+template <int N, int SIZE>
+__device__ __forceinline__ void shift_words(uint32_t (&x)[N + 4], int off) {
+#pragma unroll
+  for (int i = 0; i < N + 3; ++i) x[i] = off & 4 ? x[i + 1] : x[i];
+#pragma unroll
+  for (int i = 0; i < N + 2; ++i) x[i] = off & 8 ? x[i + 2] : x[i];
+  if constexpr (SIZE == 2) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = __funnelshift_r(x[i], x[i + 1], off & 2 ? 16 : 0);
+  }
+}
+
 }  // namespace sph
