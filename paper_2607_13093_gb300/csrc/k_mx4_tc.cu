@@ -27,7 +27,7 @@
 // so it has one barrier to wait for and one to signal, issues a stage's MMAs in one
 // piece, and takes the terms of few rows as more rows of one MMA; and by what an SM
 // gets from the L2, some 54 bytes a cycle.  1024 rows x 256000 ids x 4608 in two terms
-// take 511 us, 9.4 PFLOP/s as issued.
+// take 520 us, 9.3 PFLOP/s as issued.
 //
 // PAIR: two CTAs share a tile of 256 table rows (cta_group::2): each holds its 128
 // rows of W and half of X's codes, so that a stage costs each SM half the traffic of X.
