@@ -235,10 +235,11 @@ constexpr int kSortShort = 2048;      // tokens that one CTA sorts
 constexpr int kSortBits = 9, kSortBins = 1 << kSortBits, kSortWarps = kSortThreads / 32;
 
 struct SortSmem {
-  uint32_t hist[kSortBins];       // this CTA's count of each digit (read by the cluster)
+  uint32_t hist[kSortBins];       // this CTA's count of each digit, read by the cluster: written
+                                  // once a pass, after the barrier that ended the one before
   uint32_t base[kSortBins];       // where its next element of a digit goes
   uint32_t local[kSortBins];      // the same within the current tile
-  uint32_t half[kSortBins];       // counts of the first half of the warps
+  uint32_t half[kSortBins];       // counts of the first half of the warps, then of the second
   uint32_t part[kSortWarps];
   uint16_t warp[kSortWarps][kSortBins];
   int32_t key[kSortTile];         // the tile in the order of its digits
@@ -406,9 +407,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const TableGrad a, i
           up += c[w];
         }
       }
-      if (w0) s.hist[dig] = mine;
+      if (w0) s.half[dig] = mine;        // (its only reader so far)
       __syncthreads();
-      run = w0 ? 0 : run + s.hist[dig];
+      run = w0 ? 0 : run + s.half[dig];
       if (one && !local) place(run);
       const uint32_t local_at = sum_before(run);
       if (tid < kSortBins) s.local[tid] = local_at;
