@@ -603,6 +603,7 @@ def _mx4(w: Mx4, dev) -> sph_mx4:
         raise ValueError(f"the 4-bit rows are on {codes.device} and {scales.device}, not on {dev}")
     if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
         raise ValueError("codes and scales must be uint8")
+    ld_codes, ld_scales = _ld(codes), _ld(scales)
     rows = codes.shape[0]
     if scales.shape[0] != rows:
         raise ValueError(f"{rows} rows of codes, {scales.shape[0]} of scales")
@@ -612,10 +613,9 @@ def _mx4(w: Mx4, dev) -> sph_mx4:
     if row is not None:
         _need(row, torch.float32, "row_scale")
         _dense(dev, (row, "row_scale", rows))
-    # (a single row's stride says nothing: any width that holds it)
-    return sph_mx4(codes.data_ptr(), _ld(codes) if rows > 1 else -(-codes.shape[1] // 16) * 16,
-                   scales.data_ptr(), _ld(scales) if rows > 1 else -(-scales.shape[1] // 16) * 16,
-                   _ptr(row), rows, d, fmt)
+    if rows == 1:      # a single row's stride says nothing: any width that holds it
+        ld_codes, ld_scales = -(-codes.shape[1] // 16) * 16, -(-scales.shape[1] // 16) * 16
+    return sph_mx4(codes.data_ptr(), ld_codes, scales.data_ptr(), ld_scales, _ptr(row), rows, d, fmt)
 
 
 def _rows(t, name, dev=None):
