@@ -97,6 +97,18 @@ __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&r)[N]) 
         "r"(r[30]), "r"(r[31])
         : "memory");
 }
+// One column of this warp's lanes, read and written.
+__device__ __forceinline__ float tmem_ld1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+  return __uint_as_float(r);
+}
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(__float_as_uint(v))
+               : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
 // X's scales of a stage, one row after another in shared memory (4 G bytes each), to
 // tensor memory: word q of row r goes to lane r % 32 of column q * 4 C + r / 32.
 // (What rows past `rows` get is read by no MMA.)
@@ -307,6 +319,27 @@ struct Work {
     return true;
   }
 };
+
+// The row scales of W and X may be as far apart as 2^116 and 2^-110, and a sum is a multiple
+// of 2^-20 below 2^45: times a W scale above this it may pass fp32's range where the logit
+// does not.
+constexpr float kFarScale = 0x1p80f;
+// A warp that has such a row of W scales its tile's sums here, where they are, the further
+// terms' added (W scales above 1 after X's, others before: exactly, as 2^-130 is a step of
+// fp32), and goes on with scales of 1; what a cut tile leaves is scaled then.  Not in the
+// unrolled code of every tile: the choice there, or one product more a value, made all calls
+// longer (1024 rows x 256000 ids x 4608 525 us, 562 and 547).
+__device__ __noinline__ void scale_far_sums(uint32_t t, int bn, int acc_cols, int rows, float ws,
+                                            const float* x_row) {
+  for (int i = 0; i < rows; ++i) {
+    float v = tmem_ld1(t + i);
+    for (int c = bn; c < acc_cols; c += bn) {
+      v += tmem_ld1(t + c + i);
+      tmem_st1(t + c + i, 0.f);
+    }
+    tmem_st1(t + i, v * (ws < 1.f ? ws : 1.f) * x_row[i] * (ws < 1.f ? 1.f : ws));
+  }
+}
 
 template <int FMT, bool GATHER, bool PAIR, class OT>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -745,6 +778,12 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       float* part = p.parts + half * p.bn * kM + in_tile;
       float* mine = part + (2 * unit + (k0 > 0 || work.start(unit) == (long long)tile * p.kt ? 0 : 1)) *
                                part_size;
+      if (FMT == MX4_E4M3 && __any_sync(0xFFFFFFFFu, ws > kFarScale)) {
+        scale_far_sums(t, p.bn, p.acc_cols, rows, ws, p.x_row + r0);
+        ws = 1.f;
+#pragma unroll
+        for (int m = 0; m < kMaxBn / 32; ++m) xs[m] = 1.f;
+      }
 #pragma unroll
       for (int m = 0; m < kMaxBn / 32; ++m) {
         if (32 * m >= rows) break;
