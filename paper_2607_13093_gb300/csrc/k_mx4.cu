@@ -217,7 +217,7 @@ template <class T, int FMT, int TPR, int U, bool OPERAND>
 cudaError_t launch(const Mx4Quant& a, cudaStream_t st) {
   constexpr int kThreads = TPR < 128 ? 128 : TPR, kRows = kThreads / TPR;
   return launch_pdl(quant_kernel<T, FMT, TPR, U, OPERAND>,
-                    dim3((unsigned)((a.rows + kRows - 1) / kRows)), dim3(kThreads), 0, st, a);
+                    dim3((unsigned)(((int64_t)a.rows + kRows - 1) / kRows)), dim3(kThreads), 0, st, a);
 }
 // Hidden states are few, and the product waits for them: one step a thread and as
 // many threads as a row has, up to 512 (128 / 512 threads, the product and all, us: 32 x
