@@ -58,3 +58,33 @@ def test_bias_is_added_to_the_scaled_sum(sph, ctx):  # noqa: F811
     bound = product_bound(f64(h), table, "e4m3", 2, None, torch.float32) + \
         HALF_ULP[torch.float32] * 1.01 * (np.abs(f64(bias)) + np.abs(want))
     assert_close(y, want, bound, "bias")
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e8m0"])
+@pytest.mark.parametrize("schedule", [1, 2])
+@pytest.mark.parametrize("planes", [1, 2, 4])
+def test_finite_where_the_magnitudes_add_up_within_range(sph, ctx, fmt, schedule, planes):  # noqa: F811
+    # both formats: whatever order the products add in, no part of such a sum leaves the range
+    # (terms after the first hold less than a fourth of it); results below the normal range may
+    # be off by its start
+    V, d, R = 300, 320, 40
+    rng = np.random.default_rng(10 + planes)
+    w_exp, h_exp = rng.integers(-115, 124, V), rng.integers(-115, 124, R)
+    x = rng.standard_normal((V, d)) * 2.0 ** w_exp[:, None]
+    w = ctx.mx4_quantize(torch.tensor(x, dtype=torch.float32, device=DEV),
+                         sph.SPH_MX4_E4M3 if fmt == "e4m3" else sph.SPH_MX4_E8M0)
+    table = decoded(w, fmt)
+    h = torch.tensor(rng.standard_normal((R, d)) * 2.0 ** h_exp[:, None], dtype=torch.float32, device=DEV)
+    ctx.set_option(sph.SPH_OPT_TC_PAIR, 2)
+    ctx.set_option(sph.SPH_OPT_TC_SCHEDULE, schedule)
+    try:
+        y = f64(ctx.mx4_logits(h, w, planes=planes))
+        ctx.sync()
+    finally:
+        ctx.set_option(sph.SPH_OPT_TC_PAIR, 0)
+        ctx.set_option(sph.SPH_OPT_TC_SCHEDULE, 0)
+    want = ora.product(f64(h), table, fmt, planes)
+    sure = 2 * np.abs(f64(h)) @ np.abs(table).T < 2.0 ** 127
+    assert 0.4 < sure.mean() < 0.9
+    bound = product_bound(f64(h), table, fmt, planes, None, torch.float32) + 2.0 ** -126
+    assert_close(np.where(sure, y, 0), np.where(sure, want, 0), bound, fmt)
