@@ -1,6 +1,6 @@
 """Speculative decode steps around a vocabulary table held in 4 bits.
 
-One table serves the head, the next step's inputs and the adaptation step:
+One table serves the head, the next step's inputs and a training step of its own:
 
   quantise    the table's rows into 4 bits, once
   lookup      the inputs of the step's rows from their tokens
@@ -54,7 +54,7 @@ def run(V=32000, d=1024, sessions=8, k=4, keep_fraction=0.4, steps=3, seed=0):
         # the next step's rows: the token just drawn, then greedy drafts
         best = keep[z.view(sessions, k + 1, -1)[:, :k].argmax(2)]
         tokens = torch.cat([next_token[:, None], best], 1).reshape(-1).contiguous()
-    # adaptation: the table's gradient from the gradients of the inputs, summed over the
+    # training: the table's gradient from the gradients of the inputs, summed over the
     # occurrences of a token; the second call adds to the first
     grad = torch.empty(V, d, device=dev)
     for i, t in enumerate(seen):

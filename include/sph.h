@@ -87,7 +87,8 @@ sph_status sph_destroy(sph_ctx* ctx);
 sph_status sph_set_stream(sph_ctx* ctx, void* cuda_stream);
 
 /* Wait for all work of the context's stream; report device-side errors
- * (SPH_ERR_TIMEOUT for a wait that gave up, SPH_ERR_CUDA for faults). */
+ * (SPH_ERR_TIMEOUT for a wait that gave up, SPH_ERR_INVALID_ARG for tokens
+ * outside a table, SPH_ERR_CUDA for faults). */
 sph_status sph_sync(sph_ctx* ctx);
 
 /* Human-readable detail of the last error of `ctx` ("" if none). Owned by
@@ -117,7 +118,9 @@ typedef enum sph_option {
                                1 whole vocabulary tiles per CTA, 2 contiguous
                                k-block ranges (stream-K).  sph_mx4_logits:
                                the same of its 256-column stages; automatic
-                               takes ranges for few tiles                     */
+                               takes ranges for at most 32 rows over more
+                               than 40 stages, where the tiles are at most a
+                               third of the SMs                               */
   SPH_OPT_TC_STAGES = 3,    /* tensor-core pipeline depth: 0 automatic
                                (default), else at most this many stages (>= 2) */
   SPH_OPT_TC_BLOCK_K = 4,   /* hidden-dimension elements each pipeline stage
@@ -544,10 +547,11 @@ sph_status sph_verify_draft(sph_ctx* ctx,
  *
  * The table W [V, d] that a split head multiplies with (W_h, W_l or the whole
  * of Eq. 9) is also what the next step's inputs are read from (Eq. 1, the
- * token term) and what local adaptation trains (Eq. 20's base weights).  These
- * calls hold it in 4 bits, multiply with it, look tokens up in it, and make its
- * gradient.  They follow the conventions above; the sizes they refuse are
- * d above 2^20, rows or tokens above 2^20 (quantisation: rows up to 2^31 - 1). */
+ * token term).  These calls hold it in 4 bits, multiply with it, look tokens up
+ * in it, and make the lookup's gradient, for a program that trains the table
+ * itself (the paper's adaptation, Eq. 20, leaves the base weights as they are).
+ * They follow the conventions above; the sizes they refuse are d above 2^20, rows
+ * or tokens above 2^20 (quantisation: rows up to 2^31 - 1). */
 
 /* Element type of a table's or a result's rows. */
 typedef enum sph_tab_type {
@@ -600,7 +604,8 @@ sph_status sph_mx4_quantize(sph_ctx* ctx, const void* x, sph_tab_type x_type,
  * first quantises h as sph_mx4_quantize does, each further one quantises what
  * the terms before it left over, in units of the first one's row_scale.  One
  * term is the 4-bit product; with each further one the hidden states' rounding
- * shrinks some tenfold.  Products add in fp32.
+ * shrinks some tenfold.  Products add in fp32: a logit is finite wherever the
+ * magnitudes of its products add up within fp32's range, whatever the scales.
  *   h      [rows, W->d] bf16, fp32 or fp16, row stride ld_h elements (a slice
  *          of wider rows, any start).
  *   bias   fp32 [W->rows] or NULL.  keep_ids, n_keep as for
@@ -616,7 +621,7 @@ sph_status sph_mx4_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type,
 
 /* Rows of a table by token (Eq. 1, the token term, scaled):
  *   out[t, :] = scale * table[tokens[t], :]
- * rounded once to out_type (bf16, fp32, fp16).  A token equal to padding_id
+ * in fp32, then rounded to out_type (bf16, fp32, fp16).  A token equal to padding_id
  * gives a row of zeros (so does one outside [0, V), which sph_sync reports as
  * SPH_ERR_INVALID_ARG); -1 for no padding within the vocabulary.
  *   tokens int32 [n_tokens], n_tokens >= 0;  table bf16, fp32 or fp16 [V, d],
@@ -639,8 +644,8 @@ sph_status sph_embed_mx4(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
 /* Gradient of a table from the gradients of the looked-up rows:
  *   d_table[v, :] = scale * sum over {t : tokens[t] = v} of d_out[t, :]
  * for every row v (zeros where no token is v); with accumulate != 0 the sums are
- * added to what d_table holds, and rows without a token are not touched.  Sums
- * are fp32, rounded once to table_type, and added in an order that the tokens
+ * added to what d_table holds, and rows without a token are not touched.  All of
+ * it is fp32, then rounded to table_type, and added in an order that the tokens
  * alone decide: equal inputs give equal bits.  Tokens equal to padding_id take
  * no part (nor do ones outside [0, V), which sph_sync reports).
  *   d_out [n_tokens, d] bf16, fp32 or fp16, row stride ld_d_out;  d_table

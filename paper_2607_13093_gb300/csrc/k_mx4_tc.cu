@@ -8,8 +8,8 @@
 // states its N, and all terms of X meet a stage of W, so a term costs its MMAs
 // and no traffic of W.  The first two terms add into one accumulator, the third and
 // fourth into another: an MMA drops what lies below its accumulator's 24 bits, which
-// two terms mostly fit and four do not (300 rows x 5000 ids x 4608, four terms in one
-// accumulator: 3e-6 off, in two 6e-8).
+// two terms mostly fit and four do not (300 rows x 4608, four terms in one accumulator:
+// 3e-6 off in norm, in two 5e-8).
 //
 // A CTA keeps a ring of stages of 256 columns, 128 bytes of codes a row: codes by
 // TMA, rows of W whose kept ids are not consecutive by cp.async; X's scales by TMA,
@@ -22,12 +22,14 @@
 // queue: 1024 rows x 256000 ids x 4608 907 us.)
 //
 // Few rows are bound by the stream of W: 8 rows x 152064 ids x 7168 take 91.5 us,
-// 6.7 TB/s of the table's 4.5 bits an element.  Many rows are bound by the MMA warp's
-// own time a stage, some 560 cycles whatever the rows (waits, descriptors, the commit),
-// so it has one barrier to wait for and one to signal, issues a stage's MMAs in one
-// piece, and takes the terms of few rows as more rows of one MMA; and by what an SM
-// gets from the L2, some 54 bytes a cycle.  1024 rows x 256000 ids x 4608 in two terms
-// take 520 us, 9.3 PFLOP/s as issued.
+// 6.7 TB/s of the table's 4.5 bits an element.  Many rows are bound by what an SM gets
+// from the L2, some 54 bytes a cycle: 1024 rows x 256000 ids x 4608 in one term come in
+// tiles of 208 rows, whose stages of 48 KB, more than half of it X, take some 900 cycles
+// each; the call takes 526 us, 4.6 PFLOP/s.  The MMA warp's own time a stage, some 560
+// cycles whatever the rows (waits, descriptors, the commit), lies behind that, and shows
+// where a stage is small (32 rows x 12000 ids x 3840 9.9 us: 15 stages one after another).
+// So that warp has one barrier to wait for and one to signal, issues a stage's MMAs in
+// one piece, and takes the terms of few rows as more rows of one MMA.
 //
 // PAIR: two CTAs share a tile of 256 table rows (cta_group::2): each holds its 128
 // rows of W and half of X's codes, so that a stage costs each SM half the traffic of X.
@@ -489,8 +491,9 @@ mx4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       const int j0 = first_row(tile);
       int4 id;
       unsigned solid = 0;
-      // where rows lane / 8, lane / 8 + 4, ... begin (ids outside the table take a row of
-      // it; their scales are zeros)
+      // where rows lane / 8, lane / 8 + 4, ... begin (ids outside the table, which are the
+      // caller's mistake, take the codes of a row of it, with scale bytes of 0: 0 in e4m3,
+      // 2^-127 in e8m0)
       const uint8_t* from[kPieces ? 32 : 1];
       if constexpr (GATHER) id = ids_of(tile, solid);
       if constexpr (kPieces) {

@@ -697,7 +697,9 @@ def sph_mx4_logits(ctx, h, W: Mx4, *, keep_ids=None, bias=None, planes=2, out=No
 
 def sph_embed(ctx, tokens, table, *, scale=1.0, padding_id=-1, out=None, dtype=None):
     """scale * table[tokens] as [T, d]: tokens int32 [T], table a tensor [V, d]
-    (bf16, fp32 or fp16) or an Mx4.  dtype: the table's own, bf16 for an Mx4."""
+    (bf16, fp32 or fp16) or an Mx4.  dtype: the table's own, bf16 for an Mx4.
+    Nothing is recorded for autograd: a table that requires a gradient gets it from
+    sph_embed_grad."""
     r = _fast.embed(_word(ctx), tokens, table, scale, padding_id, out, dtype)
     if type(r) is not int:
         return r
