@@ -101,7 +101,7 @@ const char* sph_status_string(sph_status status);
 /* Pre-size the context's scratch for calls up to these sizes so that later
  * calls allocate nothing (required before capturing calls into a CUDA
  * graph).  max_d is the largest of d_h and d_l (and of the d of the operators
- * on a vocabulary table; their tokens count as rows). */
+ * on a vocabulary table and on rows; their tokens count as rows). */
 sph_status sph_reserve(sph_ctx* ctx, int64_t max_rows, int64_t max_n_keep,
                        int64_t max_d);
 
@@ -169,7 +169,8 @@ typedef enum sph_option {
                                cannot be scheduled);
                                2: never.  sph_mx4_logits too, 0: for more
                                than 96 rows in two terms or more, with kept
-                               ids in four.  The results are the fp32 sums of
+                               ids in four.  sph_fp8_logits: 1 always, else
+                               never.  The results are the fp32 sums of
                                the same products either way.               */
   SPH_OPT_SPLIT_QUANTIZE = 10, /* sph_split_step with one payload chunk: 0
                                automatic (default: in the endpoint's epilogue
@@ -255,6 +256,7 @@ enum {
   SPH_PROF_VERIFY = 4,      /* speculative acceptance                        */
   SPH_PROF_PREP = 5,        /* operand preparation (hidden-state splits)     */
   SPH_PROF_TABLE = 6,       /* operators on a vocabulary table               */
+  SPH_PROF_ROWS = 7,        /* layer norm and its gradient, shaped logits    */
   SPH_PROF_CLASSES = 8
 };
 
@@ -656,6 +658,162 @@ sph_status sph_embed_grad(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
                           int64_t ld_d_out, int64_t V, int64_t d, float scale,
                           int64_t padding_id, int accumulate, void* d_table,
                           sph_tab_type table_type, int64_t ld_table);
+
+/* Rows held in e4m3 with an fp32 scale for each block of 128 columns of one row
+ * (block_rows 1) or of 128 rows (block_rows 128; device pointers, the caller's).
+ * Column c of row r stands for
+ *   e4m3(codes[r * ld_codes + c]) * scales[r / block_rows * ld_scales + c / 128]
+ * codes start on 16 bytes, ld_codes (bytes) is a multiple of 16 and at least d;
+ * ld_scales (elements) is at least ceil(d / 128).  Nothing past column d - 1 or the
+ * last block is read or written. */
+typedef struct sph_fp8 {
+  void* codes;
+  int64_t ld_codes;
+  float* scales;
+  int64_t ld_scales;
+  int64_t rows;
+  int64_t d;
+  int32_t block_rows;       /* 1 or 128                                      */
+} sph_fp8;
+
+/* Quantise x [out->rows, out->d] (bf16, fp32 or fp16, row stride ld_x elements)
+ * into *out:
+ *   scale = max(amax / 448, 2^-126) rounded to fp32, amax the block's largest
+ *           magnitude
+ *   code  = the e4m3 value nearest to x / scale, ties to the even code
+ * A block that holds a NaN or an infinity gets a NaN scale and codes of zero, and
+ * stands for NaN throughout.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sph_status sph_fp8_quantize(sph_ctx* ctx, const void* x, sph_tab_type x_type,
+                            int64_t ld_x, const sph_fp8* out);
+
+/* sph_embed from a table held so.  tokens NULL takes its first n_tokens rows in
+ * order, whatever padding_id is (with scale 1: the values that the table stands
+ * for, rounded to fp32 and to out_type). */
+sph_status sph_embed_fp8(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
+                         const sph_fp8* table, float scale, int64_t padding_id,
+                         void* out, sph_tab_type out_type, int64_t ld_out);
+
+/* Logits over the kept rows of a table held in e4m3 blocks:
+ *   out[r, j] = sum over blocks b of sx[r, b] * sw[keep_ids[j], b]
+ *               * sum over c in b of qx[r, c] * qw[keep_ids[j], c]  (+ bias[keep_ids[j]])
+ * where qx, sx are h quantised as sph_fp8_quantize does with block_rows 1, and qw,
+ * sw the table's codes and scales.  A block's sum and the sum over blocks are
+ * fp32: a logit is finite wherever the magnitudes of its products add up within
+ * fp32's range, whatever the scales.
+ *   h      [rows, W->d] bf16, fp32 or fp16, row stride ld_h elements.
+ *   bias   fp32 [W->rows] or NULL.  keep_ids, n_keep as for
+ *          sph_partial_logits, with V = W->rows.
+ *   out    fp32 or bf16 [rows, n_keep], row stride ld_out elements.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA, OOM. */
+sph_status sph_fp8_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type,
+                          int64_t rows, int64_t ld_h, const sph_fp8* W,
+                          const float* bias, const int32_t* keep_ids,
+                          int64_t n_keep, void* out, sph_tab_type out_type,
+                          int64_t ld_out);
+
+/* ---- operators on rows ---------------------------------------------------
+ *
+ * What stands beside the head's product in a step: the norm of the hidden states
+ * before it, with its gradient for a program that trains, and the logits' way to
+ * a token after it. */
+
+/* Layer norm of each row:
+ *   out[r, c] = (x[r, c] - mean[r]) * rstd[r] * weight[c] + bias[c]
+ *   mean[r]   = sum_c x[r, c] / d, or 0 with centre == 0 (root mean square norm)
+ *   rstd[r]   = 1 / sqrt(sum_c (x[r, c] - mean[r])^2 / d + eps)
+ * in fp32, then rounded to out_type.
+ *   x      [rows, d] bf16, fp32 or fp16, row stride ld_x elements; 0 <= rows <
+ *          2^31, d <= 2^20.  The squares of a row add up within fp32's range.
+ *   weight, bias  [d] of param_type (bf16, fp32 or fp16), each or NULL (1 and 0).
+ *   eps    >= 0 and finite.
+ *   out    [rows, d], row stride ld_out; may be x itself.
+ *   mean, rstd    fp32 [rows] (out), what sph_layer_norm_grad takes, or NULL.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+sph_status sph_layer_norm(sph_ctx* ctx, const void* x, sph_tab_type x_type,
+                          int64_t rows, int64_t d, int64_t ld_x,
+                          const void* weight, const void* bias,
+                          sph_tab_type param_type, float eps, int centre,
+                          void* out, sph_tab_type out_type, int64_t ld_out,
+                          float* mean, float* rstd);
+
+/* Its gradients from d_out, the gradient of out; with n = (x - mean) * rstd and
+ * g = d_out * weight,
+ *   d_x[r, :]   = rstd[r] * (g - sum_c g / d - n * sum_c (g * n) / d)
+ *                 (the second term only where mean is given)
+ *   d_weight[c] = sum_r d_out[r, c] * n[r, c]      d_bias[c] = sum_r d_out[r, c]
+ * with accumulate != 0 the sums are added to what d_weight and d_bias hold.  All
+ * of it is fp32, then rounded to the results' types; equal inputs give equal bits.
+ *   d_out  [rows, d] bf16, fp32 or fp16, row stride ld_d_out;  x, weight as given
+ *          to sph_layer_norm.
+ *   mean, rstd  fp32 [rows], what sph_layer_norm left; mean NULL: not centred.
+ *   d_x    [rows, d], row stride ld_d_x; may be d_out or x itself.
+ *   d_weight, d_bias  [d] of grad_type (out), each or NULL.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA, OOM. */
+sph_status sph_layer_norm_grad(sph_ctx* ctx, const void* d_out,
+                               sph_tab_type d_out_type, int64_t ld_d_out,
+                               const void* x, sph_tab_type x_type, int64_t rows,
+                               int64_t d, int64_t ld_x, const void* weight,
+                               sph_tab_type weight_type, const float* mean,
+                               const float* rstd, void* d_x,
+                               sph_tab_type d_x_type, int64_t ld_d_x,
+                               void* d_weight, void* d_bias,
+                               sph_tab_type grad_type, int accumulate);
+
+/* What sph_shape_logits does to a row's logits (device pointers, all optional). */
+typedef struct sph_shaping {
+  const int32_t* history;   /* [rows, max_tokens] the row's tokens so far, its
+                               prompt's first; ids outside [0, V) mean nothing */
+  int64_t ld_history;
+  int64_t max_tokens;
+  const int32_t* lengths;   /* [rows] how many are meant (NULL: max_tokens)    */
+  const int32_t* prompt_lengths; /* [rows] how many are the prompt's (NULL: 0) */
+  const float* repetition;  /* [rows] > 0, or NULL (1)                         */
+  const float* frequency;   /* [rows] or NULL (0)                              */
+  const float* presence;    /* [rows] or NULL (0)                              */
+  const int32_t* bias_ids;  /* [rows, n_bias]; ids outside [0, V): no entry    */
+  int64_t ld_bias_ids;
+  const float* bias_values; /* [rows, n_bias]                                  */
+  int64_t ld_bias_values;
+  int64_t n_bias;
+  const uint32_t* mask;     /* [n_masks, ceil(V / 32)]: bit (v & 31) of word
+                               v >> 5 set where id v is allowed                */
+  int64_t ld_mask;
+  int64_t n_masks;
+  const int32_t* mask_rows; /* [rows] the row's mask, -1 for none (NULL: row r
+                               has mask r)                                     */
+} sph_shaping;
+
+/* Logits with penalties for repeated tokens, biases and masks, and a token:
+ *   z = logits[r, j], v = keep_ids[j]
+ *   z = z > 0 ? z / repetition[r] : z * repetition[r]    if v is among the tokens
+ *   z = z - frequency[r] * count of v, then z - presence[r]
+ *                                          if v is among those after the prompt
+ *   z = z + the sum of the row's biases for v, in the list's order
+ *   z = -infinity                          if the row's mask has v's bit clear
+ * each in fp32 and rounded; out[r, j] is z rounded to out_type.
+ * With tokens, the row's token by the rules of sph_fuse_sample: the first largest
+ * z at temperature 0, else by inverse CDF from softmax(z / temperature) with the
+ * same uniforms; -1 for a row that allows no id (every z is -infinity) or has a
+ * NaN among its z.  (Of logits that are +infinity the first is drawn at 0, each
+ * alike above.)
+ *   logits [rows, n_keep] bf16, fp32 or fp16, row stride ld_logits; rows >= 1.
+ *   keep_ids, n_keep, V  as for sph_partial_logits.
+ *   shaping  NULL for none of it.
+ *   out    [rows, n_keep], row stride ld_out; may be logits itself.  fp32 where
+ *          tokens are asked for.
+ *   tokens int32 [rows] (out) vocabulary ids, or NULL.
+ * A mask_rows entry outside [-1, n_masks) leaves the row unmasked, and sph_sync
+ * reports SPH_ERR_INVALID_ARG.  SPH_OPT_SAMPLER = 1 is not supported here.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA, OOM. */
+sph_status sph_shape_logits(sph_ctx* ctx, const void* logits,
+                            sph_tab_type logits_type, int64_t rows,
+                            int64_t ld_logits, const int32_t* keep_ids,
+                            int64_t n_keep, int64_t V,
+                            const sph_shaping* shaping, void* out,
+                            sph_tab_type out_type, int64_t ld_out,
+                            float temperature, uint64_t seed, uint64_t offset,
+                            int32_t* tokens);
 
 #ifdef __cplusplus
 }  /* extern "C" */

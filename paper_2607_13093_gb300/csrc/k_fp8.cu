@@ -1,0 +1,242 @@
+// Rows into e4m3 with a scale for each block of 128 columns, and rows of such a table back
+// (all in order, or by token).
+//
+// Bound by memory: an element is read once (2 or 4 bytes) and leaves one byte, and the other
+// way round.  A thread takes 16 consecutive columns, eight threads a block's width.  With
+// blocks of one row nothing else is shared; with blocks of 128 rows a CTA holds the whole
+// block in registers, four rows a thread, until its largest magnitude is known.
+#include <cuda_bf16.h>
+
+#include <type_traits>
+
+#include "fp8.cuh"
+#include "rows.cuh"
+#include "sm100_ptx.cuh"
+#include "sph_internal.h"
+
+namespace sph {
+namespace {
+
+constexpr int kCols = 16;                // columns of a thread
+constexpr int kLanes = kFp8Block / kCols;
+
+// A thread's 16 columns as they were read.
+template <class T>
+struct Cols16 {
+  uint4 w[sizeof(T)];
+};
+template <class T>
+__device__ __forceinline__ void load16(const T* row, int col, int d, bool aligned, Cols16<T>& r) {
+  constexpr int N = (int)sizeof(T);
+  if (col + kCols > d) {
+    T* e = reinterpret_cast<T*>(r.w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.w[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < kCols; ++j)
+      if (col + j < d) e[j] = row[col + j];
+  } else if (aligned) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.w[i] = reinterpret_cast<const uint4*>(row + col)[i];
+  } else {
+    const int off = (int)((uintptr_t)(row + col) & 15);
+    const uint4* w = reinterpret_cast<const uint4*>((uintptr_t)(row + col) - off);
+    uint32_t x[4 * N + 4];
+#pragma unroll
+    for (int i = 0; i <= N; ++i) {
+      const uint4 q = i < N || off ? w[i] : make_uint4(0, 0, 0, 0);
+      x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
+    }
+    shift_words<4 * N, N>(x, off);
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.w[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+  }
+}
+// Bits of the largest magnitude as fp32 (kFp8Inf or more: a NaN or an infinity).
+template <class T>
+__device__ __forceinline__ unsigned largest(const Cols16<T>& r) {
+  unsigned m = 0;
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(r.w);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) m = max(m, w[j] & 0x7FFFFFFFu);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kCols / 2; ++j) m = __vmaxu2(m, w[j] & 0x7FFF7FFFu);
+    m = max(m >> 16, m & 0xFFFFu);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) m <<= 16;
+    else m = m >= 0x7C00u ? kFp8Inf : __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+  }
+  return m;
+}
+template <class T>
+__device__ __forceinline__ uint4 codes16(const Cols16<T>& r, const Fp8Scale& s) {
+  const T* e = reinterpret_cast<const T*>(r.w);
+  uint32_t c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = fp8_quotient(to_f32(e[4 * i + j]), s);
+    c[i] = s.step > 0.f ? fp8_codes4(q[0], q[1], q[2], q[3]) : 0u;
+  }
+  return make_uint4(c[0], c[1], c[2], c[3]);
+}
+// Codes of columns col .. col + 15, those past d left as they are.
+__device__ __forceinline__ void store16(uint8_t* row, int col, int d, uint4 c) {
+  if (col + kCols <= d) {
+    *reinterpret_cast<uint4*>(row + col) = c;
+  } else {
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int j = 0; j < kCols; ++j)
+      if (col + j < d) row[col + j] = (uint8_t)(w[j / 4] >> 8 * (j % 4));
+  }
+}
+
+// Blocks of one row: a warp takes four blocks, `spans` of them a row.
+constexpr int kRowThreads = 256;
+template <class T>
+__global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const Fp8Quant a) {
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int64_t item = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  const int64_t row = item / a.spans;
+  if (row >= a.rows) return;
+  const int col = (int)(item - row * a.spans) * 32 * kCols + lane * kCols;
+  Cols16<T> r;
+  if (col < a.d) load16<T>(static_cast<const T*>(a.x) + row * a.ld_x, col, a.d, a.aligned != 0, r);
+  unsigned m = col < a.d ? largest<T>(r) : 0u;
+#pragma unroll
+  for (int o = 1; o < kLanes; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  if (col >= a.d) return;
+  const Fp8Scale s = fp8_scale(m);
+  store16(a.codes + row * a.ld_codes, col, a.d, codes16<T>(r, s));
+  if (col % kFp8Block == 0) a.scales[row * a.row_step + col / kFp8Block * a.col_step] = s.scale;
+}
+
+// Blocks of 128 rows: a CTA a block.
+constexpr int kTileThreads = 256;
+template <class T>
+__global__ void __launch_bounds__(kTileThreads) fp8_tiles_kernel(const Fp8Quant a) {
+  constexpr int kTurns = kFp8Block / (kTileThreads / kLanes);      // rows of a thread
+  __shared__ unsigned s_max[kTileThreads / 32];
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  const int64_t tile = blockIdx.x / a.spans;
+  const int cb = (int)(blockIdx.x - tile * a.spans);
+  const int col = cb * kFp8Block + (int)(threadIdx.x % kLanes) * kCols;
+  const int64_t row0 = tile * kFp8Block + threadIdx.x / kLanes;
+  Cols16<T> r[kTurns];
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int64_t row = row0 + i * (kTileThreads / kLanes);
+    if (row < a.rows && col < a.d)
+      load16<T>(static_cast<const T*>(a.x) + row * a.ld_x, col, a.d, a.aligned != 0, r[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i)
+    if (row0 + i * (kTileThreads / kLanes) < a.rows && col < a.d) m = max(m, largest<T>(r[i]));
+  m = __reduce_max_sync(0xFFFFFFFFu, m);
+  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kTileThreads / 32; ++w) m = max(m, s_max[w]);
+  const Fp8Scale s = fp8_scale(m);
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int64_t row = row0 + i * (kTileThreads / kLanes);
+    if (row < a.rows && col < a.d) store16(a.codes + row * a.ld_codes, col, a.d, codes16<T>(r[i], s));
+  }
+  if (threadIdx.x == 0) a.scales[tile * a.row_step + cb * a.col_step] = s.scale;
+}
+
+template <class T>
+cudaError_t launch_quant(Fp8Quant a, cudaStream_t st) {
+  if (a.block_rows == 1) {
+    a.spans = (a.d + 32 * kCols - 1) / (32 * kCols);
+    const int64_t items = a.rows * a.spans;
+    return launch_pdl(fp8_rows_kernel<T>, dim3((unsigned)((items + kRowThreads / 32 - 1) / (kRowThreads / 32))),
+                      dim3(kRowThreads), 0, st, a);
+  }
+  a.spans = (a.d + kFp8Block - 1) / kFp8Block;
+  const int64_t tiles = (a.rows + kFp8Block - 1) / kFp8Block * a.spans;
+  return launch_pdl(fp8_tiles_kernel<T>, dim3((unsigned)tiles), dim3(kTileThreads), 0, st, a);
+}
+
+// ---------------------------------------------------------------------------
+// rows back
+// ---------------------------------------------------------------------------
+// A warp takes 512 columns of a row: 16 codes a thread, two store pieces of eight.
+constexpr int kLookThreads = 128;
+template <class OT, bool ON16>
+__global__ void __launch_bounds__(kLookThreads) fp8_lookup_kernel(const Fp8Lookup a) {
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  const int64_t item = (int64_t)blockIdx.x * (kLookThreads / 32) + (threadIdx.x >> 5);
+  const int64_t t = item / a.spans;
+  if (t >= a.n) return;
+  const int span = (int)(item - t * a.spans), lane = threadIdx.x & 31;
+  const int64_t id = a.tokens ? a.tokens[t] : t;
+  const bool there = id >= 0 && id < a.V && id != a.padding;
+  if (!there && id != a.padding && span == 0 && lane == 0) atomicOr(a.status, ERR_BAD_INDEX);
+  const int col = span * 32 * kCols + lane * kCols;
+  if (col >= a.d) return;
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[h][j] = 0.f;
+  if (there) {
+    const uint8_t* row = a.codes + id * a.ld_codes;
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (col + kCols <= a.d) {
+      const uint4 c = *reinterpret_cast<const uint4*>(row + col);
+      w[0] = c.x; w[1] = c.y; w[2] = c.z; w[3] = c.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        if (col + j < a.d) w[j / 4] |= (uint32_t)row[col + j] << 8 * (j % 4);
+    }
+    const float s = a.scales[id / a.block_rows * a.ld_scales + col / kFp8Block];
+#pragma unroll
+    for (int j = 0; j < kCols; j += 2) {
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(
+          (__nv_fp8x2_storage_t)(w[j / 4] >> 8 * (j % 4) & 0xFFFFu), __NV_E4M3);
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+      v[j / 8][j % 8] = f.x * s * a.scale;
+      v[j / 8][j % 8 + 1] = f.y * s * a.scale;
+    }
+  }
+  OT* out = static_cast<OT*>(a.out) + t * a.ld_out;
+  store_cols<OT, ON16>(out, col, a.d, v[0]);
+  store_cols<OT, ON16>(out, col + 8, a.d, v[1]);
+}
+template <class OT>
+cudaError_t launch_look(Fp8Lookup a, cudaStream_t st) {
+  a.spans = (a.d + 32 * kCols - 1) / (32 * kCols);
+  const int64_t items = a.n * a.spans;
+  const dim3 grid((unsigned)((items + kLookThreads / 32 - 1) / (kLookThreads / 32)));
+  return on16(a.out, a.ld_out, (int)sizeof(OT))
+             ? launch_pdl(fp8_lookup_kernel<OT, true>, grid, dim3(kLookThreads), 0, st, a)
+             : launch_pdl(fp8_lookup_kernel<OT, false>, grid, dim3(kLookThreads), 0, st, a);
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_quant(Fp8Quant a, int x_type, cudaStream_t st) {
+  a.aligned = on16(a.x, a.ld_x, type_size(x_type));
+  if (x_type == TAB_FP32) return launch_quant<float>(a, st);
+  if (x_type == TAB_BF16) return launch_quant<__nv_bfloat16>(a, st);
+  return launch_quant<__half>(a, st);
+}
+
+cudaError_t launch_fp8_lookup(const Fp8Lookup& a, int out_type, cudaStream_t st) {
+  if (out_type == TAB_FP32) return launch_look<float>(a, st);
+  if (out_type == TAB_BF16) return launch_look<__nv_bfloat16>(a, st);
+  return launch_look<__half>(a, st);
+}
+
+}  // namespace sph

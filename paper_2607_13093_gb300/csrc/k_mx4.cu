@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "mx4.cuh"
+#include "rows.cuh"
 #include "sm100_ptx.cuh"
 #include "sph_internal.h"
 

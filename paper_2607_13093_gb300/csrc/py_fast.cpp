@@ -1,5 +1,5 @@
 // Native argument marshalling of the hot-path calls and the operators on a
-// vocabulary table for the Python binding: unpack the tensors, make the checks
+// vocabulary table and on rows for the Python binding: unpack the tensors, make the checks
 // the binding makes, call the library.  The same checks in Python and a ctypes call cost 7-8 us a call,
 // which for few rows is longer than the kernels: a step of one row x 2048
 // kept ids (two calls, 13.7 us of device time) took 25.7 us from Python and
@@ -18,6 +18,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -36,6 +37,12 @@ decltype(&sph_mx4_logits) p_mx4_logits = nullptr;
 decltype(&sph_embed) p_embed = nullptr;
 decltype(&sph_embed_mx4) p_embed_mx4 = nullptr;
 decltype(&sph_embed_grad) p_embed_grad = nullptr;
+decltype(&sph_fp8_quantize) p_fp8_quantize = nullptr;
+decltype(&sph_embed_fp8) p_embed_fp8 = nullptr;
+decltype(&sph_fp8_logits) p_fp8_logits = nullptr;
+decltype(&sph_layer_norm) p_layer_norm = nullptr;
+decltype(&sph_layer_norm_grad) p_layer_norm_grad = nullptr;
+decltype(&sph_shape_logits) p_shape_logits = nullptr;
 
 // One call's arguments; ok turns false at the first that is not plain.
 struct Args {
@@ -151,6 +158,80 @@ struct Args {
     *w = sph_mx4{c->data_ptr(), c->stride(0), s->data_ptr(), s->stride(0),
                  r ? static_cast<float*>(r->data_ptr()) : nullptr, c->size(0), dv, (int32_t)fv};
     return true;
+  }
+  // rows in e4m3 blocks: the binding's tuple (codes, scales, block_rows)
+  bool fp8(int i, sph_fp8* w) {
+    PyObject* o = a[i];
+    if (!ok || !PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) return ok = false;
+    const at::Tensor* c = tensor_of(PyTuple_GET_ITEM(o, 0));
+    const at::Tensor* s = tensor_of(PyTuple_GET_ITEM(o, 1));
+    PyObject* b = PyTuple_GET_ITEM(o, 2);
+    if (!ok || c->dim() != 2 || s->dim() != 2 ||
+        (c->scalar_type() != c10::kFloat8_e4m3fn && c->scalar_type() != c10::kByte) ||
+        s->scalar_type() != c10::kFloat || c->size(0) < 2 || c->size(1) < 1 || c->stride(1) != 1 ||
+        (s->stride(1) != 1 && s->size(1) > 1) || !PyLong_CheckExact(b))
+      return ok = false;
+    const long long block = PyLong_AsLongLong(b);
+    if (PyErr_Occurred()) { PyErr_Clear(); return ok = false; }
+    if (block != 1 && block != 128) return ok = false;
+    const long long rows = c->size(0), d = c->size(1);
+    if (s->size(0) != (rows + block - 1) / block || s->size(1) != (d + 127) / 128) return ok = false;
+    *w = sph_fp8{c->data_ptr(), c->stride(0), static_cast<float*>(s->data_ptr()),
+                 s->size(0) > 1 ? (long long)s->stride(0) : std::max<long long>(s->stride(0), s->size(1)),
+                 rows, d, (int32_t)block};
+    return true;
+  }
+  // a contiguous vector of d parameters (None: nullptr) and its type
+  void* vector(int i, long long d, sph_tab_type* type) {
+    if (!ok || a[i] == Py_None) return nullptr;
+    const at::Tensor* t = tensor(i);
+    if (!t || t->dim() != 1 || t->size(0) != d || !t->is_contiguous()) { ok = false; return nullptr; }
+    switch (t->scalar_type()) {
+      case c10::kBFloat16: *type = SPH_TAB_BF16; break;
+      case c10::kFloat: *type = SPH_TAB_FP32; break;
+      case c10::kHalf: *type = SPH_TAB_FP16; break;
+      default: ok = false; return nullptr;
+    }
+    return t->data_ptr();
+  }
+  // a contiguous vector with an element a row (None: nullptr)
+  template <class T>
+  T* per_row(int i, c10::ScalarType type, long long rows) {
+    if (!ok || a[i] == Py_None) return nullptr;
+    const at::Tensor* t = tensor(i);
+    if (!t || t->scalar_type() != type || t->dim() != 1 || t->size(0) != rows || !t->is_contiguous()) {
+      ok = false;
+      return nullptr;
+    }
+    return static_cast<T*>(t->data_ptr());
+  }
+  // a 2-D operand with a list a row (rows < 0: any number of them)
+  template <class T>
+  T* lists(int i, c10::ScalarType type, long long rows, int64_t* n, int64_t* cols, int64_t* ld) {
+    if (!ok || a[i] == Py_None) return nullptr;
+    const at::Tensor* t = tensor(i);
+    if (!t || t->scalar_type() != type || t->dim() != 2 || (t->stride(1) != 1 && t->size(1) > 1) ||
+        (rows >= 0 && t->size(0) != rows)) {
+      ok = false;
+      return nullptr;
+    }
+    *n = t->size(0);
+    *cols = t->size(1);
+    *ld = *n > 1 ? (int64_t)t->stride(0) : std::max<int64_t>(t->stride(0), *cols);
+    return static_cast<T*>(t->data_ptr());
+  }
+  bool truth(int i) {
+    if (a[i] != Py_True && a[i] != Py_False) ok = false;
+    return a[i] == Py_True;
+  }
+  // the type asked for, `fallback` for None
+  c10::ScalarType type_or(int i, c10::ScalarType fallback) {
+    if (a[i] == Py_None) return fallback;
+    if (!THPDtype_Check(a[i])) { ok = false; return fallback; }
+    return reinterpret_cast<THPDtype*>(a[i])->scalar_type;
+  }
+  at::TensorOptions on(c10::ScalarType type) const {
+    return at::TensorOptions().dtype(type).device(c10::kCUDA, (int8_t)dev);
   }
   // the result: the given tensor of shape [n, d], or a new one of the type asked for
   // (fallback where none is); `made` keeps a new one alive
@@ -431,6 +512,15 @@ PyObject* embed(PyObject*, PyObject* const* argv, Py_ssize_t n) {
     const long long padding = A.integer(4);
     if (!A.ok || !ctx) return not_taken();
     at::Tensor made;
+    if (PyTuple_Check(argv[2]) && PyTuple_GET_SIZE(argv[2]) == 3) {
+      sph_fp8 w{};
+      if (!A.fp8(2, &w)) return not_taken();
+      const Args::Rows o = A.result(5, 6, c10::kBFloat16, t->numel(), w.d, &made);
+      if (!A.ok || o.n < 1) return not_taken();
+      return answer(unlocked([&] {
+                      return p_embed_fp8(ctx, tokens, o.n, &w, scale, padding, o.p, o.type, o.ld);
+                    }), argv[5], made);
+    }
     if (PyTuple_Check(argv[2])) {
       sph_mx4 w{};
       if (!A.mx4(2, &w)) return not_taken();
@@ -477,34 +567,259 @@ PyObject* embed_grad(PyObject*, PyObject* const* argv, Py_ssize_t n) {
   });
 }
 
+// (ctx, x, block_rows): (codes, scales)
+PyObject* fp8_quantize(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 3) return not_taken();
+    Args A{argv};
+    auto* ctx = reinterpret_cast<sph_ctx*>((uintptr_t)A.word(0));
+    const Args::Rows x = A.rows(1);
+    const long long block = A.integer(2);
+    if (!A.ok || !ctx || x.n < 1 || x.d < 1 || x.d > (1 << 20) || (block != 1 && block != 128))
+      return not_taken();
+    at::Tensor codes = at::empty_strided({x.n, x.d}, {(x.d + 15) / 16 * 16, 1}, A.on(c10::kFloat8_e4m3fn));
+    at::Tensor scales = at::empty({(x.n + block - 1) / block, (x.d + 127) / 128}, A.on(c10::kFloat));
+    const sph_fp8 w{codes.data_ptr(), (x.d + 15) / 16 * 16, static_cast<float*>(scales.data_ptr()),
+                    scales.size(1), x.n, x.d, (int32_t)block};
+    const sph_status st = unlocked([&] { return p_fp8_quantize(ctx, x.p, x.type, x.ld, &w); });
+    if (st != SPH_OK) return outcome(st, 0);
+    PyObject* c = THPVariable_Wrap(codes);
+    PyObject* s = THPVariable_Wrap(scales);
+    PyObject* t = c && s ? PyTuple_Pack(2, c, s) : nullptr;
+    Py_XDECREF(c);
+    Py_XDECREF(s);
+    return t;
+  });
+}
+
+// (ctx, w, out, dtype)
+PyObject* fp8_dequantize(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 4) return not_taken();
+    Args A{argv};
+    auto* ctx = reinterpret_cast<sph_ctx*>((uintptr_t)A.word(0));
+    sph_fp8 w{};
+    if (!A.fp8(1, &w) || !ctx) return not_taken();
+    at::Tensor made;
+    const Args::Rows o = A.result(2, 3, c10::kBFloat16, w.rows, w.d, &made);
+    if (!A.ok) return not_taken();
+    return answer(unlocked([&] {
+                    return p_embed_fp8(ctx, nullptr, w.rows, &w, 1.f, -1, o.p, o.type, o.ld);
+                  }), argv[2], made);
+  });
+}
+
+// (ctx, h, W, keep_ids, bias, out, dtype)
+PyObject* fp8_logits(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 7) return not_taken();
+    Args A{argv};
+    auto* ctx = reinterpret_cast<sph_ctx*>((uintptr_t)A.word(0));
+    const Args::Rows h = A.rows(1);
+    sph_fp8 w{};
+    if (!A.fp8(2, &w) || !ctx || h.d != w.d) return not_taken();
+    const int32_t* keep = A.dense<int32_t>(3, c10::kInt, 0);
+    const long long nk = A.none(3) ? w.rows : A.ok ? (long long)THPVariable_Unpack(argv[3]).numel() : 0;
+    const float* bias = A.dense<float>(4, c10::kFloat, w.rows);
+    if (!A.ok || nk < 1) return not_taken();
+    at::Tensor made;
+    const Args::Rows o = A.result(5, 6, c10::kFloat, h.n, nk, &made);
+    if (!A.ok) return not_taken();
+    return answer(unlocked([&] {
+                    return p_fp8_logits(ctx, h.p, h.type, h.n, h.ld, &w, bias, keep, nk, o.p, o.type, o.ld);
+                  }), argv[5], made);
+  });
+}
+
+// A new reference to the given object, or to a new tensor's (None where there is neither).
+PyObject* given_or(PyObject* given, const at::Tensor& made) {
+  if (made.defined()) return THPVariable_Wrap(made);
+  Py_INCREF(given);
+  return given;
+}
+PyObject* triple(PyObject* a, PyObject* b, PyObject* c) {
+  PyObject* t = a && b && c ? PyTuple_Pack(3, a, b, c) : nullptr;
+  Py_XDECREF(a);
+  Py_XDECREF(b);
+  Py_XDECREF(c);
+  return t;
+}
+
+// (ctx, x, weight, bias, eps, centre, stats, out, dtype): out, or (out, mean, rstd)
+PyObject* layer_norm(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 9) return not_taken();
+    Args A{argv};
+    auto* ctx = reinterpret_cast<sph_ctx*>((uintptr_t)A.word(0));
+    const Args::Rows x = A.rows(1);
+    sph_tab_type wt = SPH_TAB_BF16, bt = SPH_TAB_BF16;
+    const void* w = A.vector(2, x.d, &wt);
+    const void* b = A.vector(3, x.d, &bt);
+    const float eps = A.real(4);
+    const bool centre = A.truth(5), stats = A.truth(6);
+    if (!A.ok || !ctx || (w && b && wt != bt)) return not_taken();
+    at::Tensor made, mean, rstd;
+    const Args::Rows o = A.result(7, 8, x.t->scalar_type(), x.n, x.d, &made);
+    if (!A.ok) return not_taken();
+    if (stats) {
+      rstd = at::empty({x.n}, A.on(c10::kFloat));
+      if (centre) mean = at::empty({x.n}, A.on(c10::kFloat));
+    }
+    float* const m = mean.defined() ? static_cast<float*>(mean.data_ptr()) : nullptr;
+    float* const r = rstd.defined() ? static_cast<float*>(rstd.data_ptr()) : nullptr;
+    const sph_status st = unlocked([&] {
+      return p_layer_norm(ctx, x.p, x.type, x.n, x.d, x.ld, w, b, w ? wt : bt, eps, centre ? 1 : 0,
+                          o.p, o.type, o.ld, m, r);
+    });
+    if (st != SPH_OK || !stats) return answer(st, argv[7], made);
+    return triple(given_or(argv[7], made), given_or(Py_None, mean), given_or(Py_None, rstd));
+  });
+}
+
+// (ctx, d_out, x, weight, mean, rstd, bias, accumulate, d_x, d_weight, d_bias, dtype,
+//  grad_dtype): (d_x, d_weight, d_bias)
+PyObject* layer_norm_grad(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 13) return not_taken();
+    Args A{argv};
+    auto* ctx = reinterpret_cast<sph_ctx*>((uintptr_t)A.word(0));
+    const Args::Rows y = A.rows(1), x = A.rows(2);
+    if (!A.ok || !ctx || x.n != y.n || x.d != y.d) return not_taken();
+    sph_tab_type wt = SPH_TAB_BF16, gt = SPH_TAB_BF16, bt = SPH_TAB_BF16;
+    const void* w = A.vector(3, x.d, &wt);
+    const float* mean = A.per_row<float>(4, c10::kFloat, x.n);
+    const float* rstd = A.per_row<float>(5, c10::kFloat, x.n);
+    const bool bias = A.truth(6), add = A.truth(7);
+    if (!A.ok || (!rstd && x.n > 0) || (add && ((w && A.none(9)) || (bias && A.none(10)))))
+      return not_taken();
+    at::Tensor made, made_w, made_b;
+    const Args::Rows o = A.result(8, 11, y.t->scalar_type(), x.n, x.d, &made);
+    const c10::ScalarType grad = A.type_or(12, c10::kFloat);
+    if (!A.ok) return not_taken();
+    void *dw = nullptr, *db = nullptr;
+    auto vector_of = [&](const at::Tensor& t, sph_tab_type* type) -> void* {
+      switch (t.scalar_type()) {
+        case c10::kBFloat16: *type = SPH_TAB_BF16; break;
+        case c10::kFloat: *type = SPH_TAB_FP32; break;
+        case c10::kHalf: *type = SPH_TAB_FP16; break;
+        default: A.ok = false;
+      }
+      return t.data_ptr();
+    };
+    if (w) {
+      if (A.none(9)) dw = vector_of(made_w = at::empty({x.d}, A.on(grad)), &gt);
+      else dw = A.vector(9, x.d, &gt);
+    }
+    if (bias) {
+      if (A.none(10)) {
+        const c10::ScalarType same =
+            !dw ? grad : gt == SPH_TAB_FP32 ? c10::kFloat : gt == SPH_TAB_BF16 ? c10::kBFloat16 : c10::kHalf;
+        db = vector_of(made_b = at::empty({x.d}, A.on(same)), &bt);
+      } else {
+        db = A.vector(10, x.d, &bt);
+      }
+    }
+    if (!A.ok || (dw && db && gt != bt)) return not_taken();
+    const sph_status st = unlocked([&] {
+      return p_layer_norm_grad(ctx, y.p, y.type, y.ld, x.p, x.type, x.n, x.d, x.ld, w, wt, mean, rstd,
+                               o.p, o.type, o.ld, dw, db, dw ? gt : bt, add ? 1 : 0);
+    });
+    if (st != SPH_OK) return outcome(st, 0);
+    return triple(given_or(argv[8], made), w ? given_or(argv[9], made_w) : given_or(Py_None, {}),
+                  bias ? given_or(argv[10], made_b) : given_or(Py_None, {}));
+  });
+}
+
+// (ctx, logits, V, keep_ids, history, lengths, prompt_lengths, repetition, frequency,
+//  presence, bias_ids, bias_values, mask, mask_rows, temperature, seed, offset, out, dtype,
+//  tokens): out, or (out, tokens)
+PyObject* shape_logits(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 20) return not_taken();
+    Args A{argv};
+    auto* ctx = reinterpret_cast<sph_ctx*>((uintptr_t)A.word(0));
+    const Args::Rows z = A.rows(1);
+    const long long V = A.integer(2);
+    const int32_t* keep = A.dense<int32_t>(3, c10::kInt, 0);
+    if (!A.ok || !ctx || z.n < 1 || z.d < 1 || V < 1 || V > INT32_MAX) return not_taken();
+    if ((A.none(3) ? V : (long long)THPVariable_Unpack(argv[3]).numel()) != z.d) return not_taken();
+    sph_shaping s{};
+    int64_t rows = 0, cols = 0;
+    s.history = A.lists<int32_t>(4, c10::kInt, z.n, &rows, &s.max_tokens, &s.ld_history);
+    s.lengths = A.per_row<int32_t>(5, c10::kInt, z.n);
+    s.prompt_lengths = A.per_row<int32_t>(6, c10::kInt, z.n);
+    s.repetition = A.per_row<float>(7, c10::kFloat, z.n);
+    s.frequency = A.per_row<float>(8, c10::kFloat, z.n);
+    s.presence = A.per_row<float>(9, c10::kFloat, z.n);
+    s.bias_ids = A.lists<int32_t>(10, c10::kInt, z.n, &rows, &s.n_bias, &s.ld_bias_ids);
+    cols = s.n_bias;
+    s.bias_values = A.lists<float>(11, c10::kFloat, z.n, &rows, &cols, &s.ld_bias_values);
+    int64_t words = 0;
+    s.mask = reinterpret_cast<uint32_t*>(A.lists<int32_t>(12, c10::kInt, -1, &s.n_masks, &words, &s.ld_mask));
+    s.mask_rows = A.per_row<int32_t>(13, c10::kInt, z.n);
+    if (!A.ok || A.none(10) != A.none(11) || cols != s.n_bias ||
+        (!A.none(12) && words < (V + 31) / 32) || (!A.none(4) && s.max_tokens < 1))
+      return not_taken();
+    const bool draw = !A.none(14);
+    const float temperature = draw ? A.real(14) : 0.f;
+    const unsigned long long seed = A.word(15), offset = A.word(16);
+    at::Tensor made, made_tokens;
+    const Args::Rows o = A.result(17, 18, z.t->scalar_type(), z.n, z.d, &made);
+    if (!A.ok || (!draw && !A.none(19))) return not_taken();
+    int32_t* tokens = nullptr;
+    if (draw) {
+      if (A.none(19)) {
+        made_tokens = at::empty({z.n}, A.on(c10::kInt));
+        tokens = static_cast<int32_t*>(made_tokens.data_ptr());
+      } else {
+        tokens = A.dense<int32_t>(19, c10::kInt, z.n);
+      }
+    }
+    if (!A.ok) return not_taken();
+    const sph_status st = unlocked([&] {
+      return p_shape_logits(ctx, z.p, z.type, z.n, z.ld, keep, z.d, V, &s, o.p, o.type, o.ld,
+                            temperature, seed, offset, tokens);
+    });
+    if (st != SPH_OK || !draw) return answer(st, argv[17], made);
+    PyObject* a = given_or(argv[17], made);
+    PyObject* b = given_or(argv[19], made_tokens);
+    PyObject* t = a && b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    return t;
+  });
+}
+
 // Find the library's calls in the libsph.so that the binding has loaded.
 PyObject* bind(PyObject*, PyObject* path) {
   const char* p = PyUnicode_AsUTF8(path);
   if (!p) return nullptr;
   void* lib = dlopen(p, RTLD_NOW | RTLD_LOCAL);
   auto find = [&](const char* name) { return lib ? dlsym(lib, name) : nullptr; };
-  const char* const names[9] = {"sph_partial_logits", "sph_fuse_sample", "sph_split_step",
-                                "sph_verify_draft", "sph_mx4_quantize", "sph_mx4_logits",
-                                "sph_embed", "sph_embed_mx4", "sph_embed_grad"};
-  void* f[9];
   bool all = true;
-  for (int i = 0; i < 9; ++i) {
-    f[i] = find(names[i]);
-    all = all && f[i];
-  }
+  auto take = [&](auto& call, const char* name) {
+    call = reinterpret_cast<std::decay_t<decltype(call)>>(find(name));
+    all = all && call;
+  };
+  take(p_partial, "sph_partial_logits");
+  take(p_fuse, "sph_fuse_sample");
+  take(p_split, "sph_split_step");
+  take(p_verify, "sph_verify_draft");
+  take(p_quantize, "sph_mx4_quantize");
+  take(p_mx4_logits, "sph_mx4_logits");
+  take(p_embed, "sph_embed");
+  take(p_embed_mx4, "sph_embed_mx4");
+  take(p_embed_grad, "sph_embed_grad");
+  take(p_fp8_quantize, "sph_fp8_quantize");
+  take(p_embed_fp8, "sph_embed_fp8");
+  take(p_fp8_logits, "sph_fp8_logits");
+  take(p_layer_norm, "sph_layer_norm");
+  take(p_layer_norm_grad, "sph_layer_norm_grad");
+  take(p_shape_logits, "sph_shape_logits");
   if (!all) {
     PyErr_Format(PyExc_RuntimeError, "the hot-path calls were not found in %s", p);
     return nullptr;
   }
-  p_partial = reinterpret_cast<decltype(p_partial)>(f[0]);
-  p_fuse = reinterpret_cast<decltype(p_fuse)>(f[1]);
-  p_split = reinterpret_cast<decltype(p_split)>(f[2]);
-  p_verify = reinterpret_cast<decltype(p_verify)>(f[3]);
-  p_quantize = reinterpret_cast<decltype(p_quantize)>(f[4]);
-  p_mx4_logits = reinterpret_cast<decltype(p_mx4_logits)>(f[5]);
-  p_embed = reinterpret_cast<decltype(p_embed)>(f[6]);
-  p_embed_mx4 = reinterpret_cast<decltype(p_embed_mx4)>(f[7]);
-  p_embed_grad = reinterpret_cast<decltype(p_embed_grad)>(f[8]);
   Py_RETURN_NONE;
 }
 
@@ -519,6 +834,12 @@ PyMethodDef methods[] = {
     {"mx4_logits", (PyCFunction)(void (*)(void))mx4_logits, METH_FASTCALL, nullptr},
     {"embed", (PyCFunction)(void (*)(void))embed, METH_FASTCALL, nullptr},
     {"embed_grad", (PyCFunction)(void (*)(void))embed_grad, METH_FASTCALL, nullptr},
+    {"fp8_quantize", (PyCFunction)(void (*)(void))fp8_quantize, METH_FASTCALL, nullptr},
+    {"fp8_dequantize", (PyCFunction)(void (*)(void))fp8_dequantize, METH_FASTCALL, nullptr},
+    {"fp8_logits", (PyCFunction)(void (*)(void))fp8_logits, METH_FASTCALL, nullptr},
+    {"layer_norm", (PyCFunction)(void (*)(void))layer_norm, METH_FASTCALL, nullptr},
+    {"layer_norm_grad", (PyCFunction)(void (*)(void))layer_norm_grad, METH_FASTCALL, nullptr},
+    {"shape_logits", (PyCFunction)(void (*)(void))shape_logits, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "py_fast", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,99 @@
+// Rows of bf16, fp32 or fp16 at any address, eight columns a thread: loads by 16-byte
+// words wherever the row starts, conversions, stores.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "sph_internal.h"
+
+namespace sph {
+
+// N words of elements of SIZE bytes that start `off` bytes into x (less than 16): moved to
+// x's start.
+template <int N, int SIZE>
+__device__ __forceinline__ void shift_words(uint32_t (&x)[N + 4], int off) {
+#pragma unroll
+  for (int i = 0; i < N + 3; ++i) x[i] = off & 4 ? x[i + 1] : x[i];
+#pragma unroll
+  for (int i = 0; i < N + 2; ++i) x[i] = off & 8 ? x[i + 2] : x[i];
+  if constexpr (SIZE == 2) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = __funnelshift_r(x[i], x[i + 1], off & 2 ? 16 : 0);
+  }
+}
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <class T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) {
+  return __float2bfloat16_rn(x);
+}
+
+// Eight consecutive elements at any address, by the 16-byte words that hold them (each of
+// which holds one of the elements at least).
+template <class T>
+__device__ __forceinline__ void load_8(const T* p, float (&v)[8]) {
+  constexpr int N = 2 * (int)sizeof(T);         // words
+  const int off = (int)((uintptr_t)p & 15);
+  const uint4* w = reinterpret_cast<const uint4*>((uintptr_t)p - off);
+  uint32_t x[N + 4];
+#pragma unroll
+  for (int i = 0; i <= N / 4; ++i) {
+    const uint4 q = i < N / 4 || off ? w[i] : make_uint4(0, 0, 0, 0);
+    x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
+  }
+  shift_words<N, sizeof(T)>(x, off);
+  const T* e = reinterpret_cast<const T*>(x);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
+}
+
+// A thread's eight columns of a row, col .. col + 7 (those in 0 .. d - 1; zeros for the
+// others).  VEC: rows and col are on 16 bytes.
+template <class T, bool VEC>
+__device__ __forceinline__ void load_cols(const T* row, int col, int d, float (&v)[8]) {
+  const bool all = (VEC || col >= 0) && col + 8 <= d;
+  if (VEC && all) {
+    uint4 w[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+      w[i] = reinterpret_cast<const uint4*>(row + col)[i];
+    const T* e = reinterpret_cast<const T*>(w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
+  } else if (all) {
+    load_8(row + col, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      v[j] = col + j >= 0 && col + j < d ? to_f32(row[col + j]) : 0.f;
+  }
+}
+// ON16: row + col is on 16 bytes.
+template <class T, bool ON16>
+__device__ __forceinline__ void store_cols(T* row, int col, int d, const float (&v)[8]) {
+  if (ON16 && col >= 0 && col + 8 <= d) {
+    uint4 w[sizeof(T) / 2];
+    T* e = reinterpret_cast<T*>(w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = from_f32<T>(v[j]);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + col)[i] = w[i];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (col + j >= 0 && col + j < d) row[col + j] = from_f32<T>(v[j]);
+  }
+}
+
+inline bool on16(const void* p, int64_t ld, int size) {
+  return ((uintptr_t)p & 15) == 0 && (ld * size & 15) == 0;
+}
+inline int type_size(int t) { return t == TAB_FP32 ? 4 : 2; }
+
+}  // namespace sph

@@ -763,6 +763,13 @@ sph_status sph_reserve(sph_ctx* ctx, int64_t max_rows, int64_t max_n_keep,
   if (m > need) need = m;
   const size_t t = sph::grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
   if (t > need) need = t;
+  const size_t q = sph::fp8_gemm_reserve_bytes(max_rows, max_d);
+  if (q > need) need = q;
+  // the operators on rows
+  const size_t n = sph::norm_grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
+  if (n > need) need = n;
+  const size_t s = sph::shape_reserve_bytes(max_rows, max_n_keep);
+  if (s > need) need = s;
   for (int act = 0; act < 2; ++act) {      // a one-chunk split step
     const size_t a = split_scratch_bytes(ctx, max_rows, max_n_keep, max_n_keep, max_d, max_d,
                                          act, sph::W_BF16);
@@ -1494,6 +1501,273 @@ sph_status sph_embed_grad(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
                          return sph::launch_table_grad(a, d_out_type, table_type, ctx->scratch,
                                                        ctx->sm_count, ctx->stream);
                        }), "table gradient launch");
+}
+
+// ---- rows in e4m3 with block scales -------------------------------------------
+namespace {
+
+sph_status check_fp8(sph_ctx* ctx, const sph_fp8* w) {
+  if (!w) return fail(ctx, SPH_ERR_INVALID_ARG, "the e4m3 rows must be non-NULL");
+  if (w->block_rows != 1 && w->block_rows != sph::kFp8Block)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "block_rows=%d must be 1 or 128", (int)w->block_rows);
+  sph_status st = check_d(ctx, w->d);
+  if (st) return st;
+  if (w->rows < 1 || w->rows > INT32_MAX)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "rows=%lld of the e4m3 form out of range", (long long)w->rows);
+  if (!w->codes || !w->scales) return fail(ctx, SPH_ERR_INVALID_ARG, "codes and scales must be non-NULL");
+  if (((uintptr_t)w->codes & 15) || (w->ld_codes & 15))
+    return fail(ctx, SPH_ERR_INVALID_ARG, "codes and their row stride must be 16-byte aligned");
+  if ((uintptr_t)w->scales & 3) return fail(ctx, SPH_ERR_INVALID_ARG, "scales are not aligned to their elements");
+  const int64_t blocks = (w->d + sph::kFp8Block - 1) / sph::kFp8Block;
+  if (w->ld_codes < w->d || w->ld_scales < blocks)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "rows of %lld columns need strides of %lld codes and %lld scales",
+                (long long)w->d, (long long)w->d, (long long)blocks);
+  if (w->ld_codes >= ((int64_t)1 << 40))
+    return fail(ctx, SPH_ERR_UNSUPPORTED, "row stride of the codes too large");
+  return SPH_OK;
+}
+
+}  // namespace
+
+sph_status sph_fp8_quantize(sph_ctx* ctx, const void* x, sph_tab_type x_type, int64_t ld_x,
+                            const sph_fp8* out) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_fp8(ctx, out);
+  if (st) return st;
+  st = check_rows(ctx, "x", x, x_type, out->d, ld_x);
+  if (st) return st;
+  if (out->rows * ((out->d + 1023) / 1024) > INT32_MAX)
+    return fail(ctx, SPH_ERR_UNSUPPORTED, "%lld rows of %lld columns in one call", (long long)out->rows,
+                (long long)out->d);
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  sph::Fp8Quant q{};
+  q.x = x; q.ld_x = ld_x; q.rows = out->rows; q.d = (int)out->d; q.block_rows = out->block_rows;
+  q.codes = static_cast<uint8_t*>(out->codes); q.ld_codes = out->ld_codes;
+  q.scales = out->scales; q.row_step = out->ld_scales; q.col_step = 1;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_fp8_quant(q, x_type, ctx->stream);
+                       }), "e4m3 quantise launch");
+}
+
+sph_status sph_embed_fp8(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
+                         const sph_fp8* table, float scale, int64_t padding_id, void* out,
+                         sph_tab_type out_type, int64_t ld_out) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_fp8(ctx, table);
+  if (st) return st;
+  if (tokens) {
+    st = check_tokens(ctx, tokens, n_tokens);
+    if (st) return st;
+  } else if (n_tokens < 0 || n_tokens > table->rows) {
+    return fail(ctx, SPH_ERR_INVALID_ARG, "n_tokens=%lld of %lld rows in order", (long long)n_tokens,
+                (long long)table->rows);
+  }
+  if (n_tokens == 0) return SPH_OK;
+  st = check_lookup(ctx, n_tokens, table->d, scale, out, out_type, ld_out);
+  if (st) return st;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  sph::Fp8Lookup a{};
+  a.tokens = tokens; a.n = n_tokens;
+  a.codes = static_cast<const uint8_t*>(table->codes); a.ld_codes = table->ld_codes;
+  a.scales = table->scales; a.ld_scales = table->ld_scales; a.V = table->rows; a.d = (int)table->d;
+  a.block_rows = table->block_rows;
+  a.scale = scale; a.padding = tokens ? padding_id : -1; a.out = out; a.ld_out = ld_out; a.status = ctx->status;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_fp8_lookup(a, out_type, ctx->stream);
+                       }), "e4m3 lookup launch");
+}
+
+sph_status sph_fp8_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type, int64_t rows,
+                          int64_t ld_h, const sph_fp8* W, const float* bias,
+                          const int32_t* keep_ids, int64_t n_keep, void* out,
+                          sph_tab_type out_type, int64_t ld_out) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_fp8(ctx, W);
+  if (st) return st;
+  st = check_rows(ctx, "h", h, h_type, W->d, ld_h);
+  if (st) return st;
+  if (rows < 1 || rows > kTabMaxRows)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "rows=%lld out of [1, 2^20]", (long long)rows);
+  st = check_ids(ctx, keep_ids, n_keep, W->rows);
+  if (st) return st;
+  if (out_type == SPH_TAB_FP16) return fail(ctx, SPH_ERR_UNSUPPORTED, "logits are fp32 or bf16");
+  st = check_rows(ctx, "out", out, out_type, n_keep, ld_out);
+  if (st) return st;
+  if (n_keep > sph::sample_max_n()) return fail(ctx, SPH_ERR_UNSUPPORTED, "n_keep above %d", sph::sample_max_n());
+  if (rows * n_keep > ((int64_t)1 << 40)) return fail(ctx, SPH_ERR_UNSUPPORTED, "rows*n_keep too large");
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  st = host_check_ids(ctx, keep_ids, n_keep, W->rows);
+  if (st) return st;
+  const sph::Fp8Plan plan{rows, n_keep, (int)W->d, ctx->sm_count, ctx->pair_units, pair_mode(ctx),
+                          keep_ids != nullptr};
+  st = ensure_scratch(ctx, sph::fp8_gemm_scratch_bytes(plan));
+  if (st) return st;
+  sph::Fp8Gemm m{};
+  m.x = h; m.ld_x = ld_h; m.rows = (int)rows; m.d = (int)W->d; m.x_type = h_type;
+  m.w_codes = static_cast<const uint8_t*>(W->codes); m.ld_codes = W->ld_codes;
+  m.w_scales = W->scales; m.ld_scales = W->ld_scales; m.block_rows = W->block_rows;
+  m.V = W->rows; m.bias = bias; m.ids = keep_ids; m.n = (int)n_keep;
+  m.out = out; m.ld_out = ld_out; m.out_type = out_type; m.status = ctx->status;
+  return launch_status(ctx, traced(ctx, SPH_PROF_TABLE, [&] {
+                         return sph::launch_fp8_gemm(m, plan, ctx->scratch, ctx->spin_limit,
+                                                     ctx->stream);
+                       }), "e4m3 product launch");
+}
+
+// ---- operators on rows --------------------------------------------------------
+namespace {
+
+// A vector of d parameters, or of their gradients, that may be left out.
+sph_status check_param(sph_ctx* ctx, const char* name, const void* p, int type) {
+  if (!p) return SPH_OK;
+  if (!tab_dense(type)) return fail(ctx, SPH_ERR_INVALID_ARG, "%s: type %d is not bf16, fp32 or fp16", name, type);
+  if ((uintptr_t)p % tab_size(type)) return fail(ctx, SPH_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+  return SPH_OK;
+}
+sph_status check_norm_rows(sph_ctx* ctx, int64_t rows, int64_t d) {
+  if (rows < 0 || rows > INT32_MAX) return fail(ctx, SPH_ERR_INVALID_ARG, "rows=%lld out of [0, 2^31)", (long long)rows);
+  return check_d(ctx, d);
+}
+
+}  // namespace
+
+sph_status sph_layer_norm(sph_ctx* ctx, const void* x, sph_tab_type x_type, int64_t rows, int64_t d,
+                          int64_t ld_x, const void* weight, const void* bias,
+                          sph_tab_type param_type, float eps, int centre, void* out,
+                          sph_tab_type out_type, int64_t ld_out, float* mean, float* rstd) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_norm_rows(ctx, rows, d);
+  if (st) return st;
+  if (!std::isfinite(eps) || eps < 0.f) return fail(ctx, SPH_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  st = check_param(ctx, "weight", weight, param_type);
+  if (!st) st = check_param(ctx, "bias", bias, param_type);
+  if (st) return st;
+  if (rows == 0) return SPH_OK;
+  st = check_rows(ctx, "x", x, x_type, d, ld_x);
+  if (!st) st = check_rows(ctx, "out", out, out_type, d, ld_out);
+  if (st) return st;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  sph::Norm a{};
+  a.x = x; a.ld_x = ld_x; a.rows = rows; a.d = (int)d;
+  a.weight = weight; a.bias = bias; a.param_type = param_type; a.eps = eps; a.centre = centre != 0;
+  a.out = out; a.out_type = out_type; a.ld_out = ld_out; a.mean = mean; a.rstd = rstd;
+  return launch_status(ctx, traced(ctx, SPH_PROF_ROWS, [&] {
+                         return sph::launch_norm(a, x_type, ctx->sm_count, ctx->stream);
+                       }), "layer norm launch");
+}
+
+sph_status sph_layer_norm_grad(sph_ctx* ctx, const void* d_out, sph_tab_type d_out_type,
+                               int64_t ld_d_out, const void* x, sph_tab_type x_type, int64_t rows,
+                               int64_t d, int64_t ld_x, const void* weight,
+                               sph_tab_type weight_type, const float* mean, const float* rstd,
+                               void* d_x, sph_tab_type d_x_type, int64_t ld_d_x, void* d_weight,
+                               void* d_bias, sph_tab_type grad_type, int accumulate) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  sph_status st = check_norm_rows(ctx, rows, d);
+  if (st) return st;
+  st = check_param(ctx, "weight", weight, weight_type);
+  if (!st) st = check_param(ctx, "d_weight", d_weight, grad_type);
+  if (!st) st = check_param(ctx, "d_bias", d_bias, grad_type);
+  if (st) return st;
+  if (rows > 0) {
+    st = check_rows(ctx, "d_out", d_out, d_out_type, d, ld_d_out);
+    if (!st) st = check_rows(ctx, "x", x, x_type, d, ld_x);
+    if (!st) st = check_rows(ctx, "d_x", d_x, d_x_type, d, ld_d_x);
+    if (st) return st;
+    if (!rstd) return fail(ctx, SPH_ERR_INVALID_ARG, "rstd must be non-NULL");
+  }
+  if (rows == 0 && (accumulate || (!d_weight && !d_bias))) return SPH_OK;
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  if (d_weight || d_bias) {
+    st = ensure_scratch(ctx, sph::norm_grad_scratch_bytes(rows, (int)d, ctx->sm_count));
+    if (st) return st;
+  }
+  sph::NormGrad a{};
+  a.dy = d_out; a.ld_dy = ld_d_out; a.x = x; a.ld_x = ld_x; a.rows = rows; a.d = (int)d;
+  a.weight = weight; a.weight_type = weight_type; a.mean = mean; a.rstd = rstd;
+  a.dx = d_x; a.dx_type = d_x_type; a.ld_dx = ld_d_x; a.dw = d_weight; a.db = d_bias;
+  a.accumulate = accumulate != 0;
+  return launch_status(ctx, traced(ctx, SPH_PROF_ROWS, [&] {
+                         return sph::launch_norm_grad(a, x_type, d_out_type, grad_type, ctx->scratch,
+                                                      ctx->sm_count, ctx->stream);
+                       }), "layer norm gradient launch");
+}
+
+sph_status sph_shape_logits(sph_ctx* ctx, const void* logits, sph_tab_type logits_type,
+                            int64_t rows, int64_t ld_logits, const int32_t* keep_ids,
+                            int64_t n_keep, int64_t V, const sph_shaping* shaping, void* out,
+                            sph_tab_type out_type, int64_t ld_out, float temperature,
+                            uint64_t seed, uint64_t offset, int32_t* tokens) {
+  if (!ctx) return SPH_ERR_INVALID_ARG;
+  if (rows < 1 || rows > kTabMaxRows)
+    return fail(ctx, SPH_ERR_INVALID_ARG, "rows=%lld out of [1, 2^20]", (long long)rows);
+  sph_status st = check_ids(ctx, keep_ids, n_keep, V);
+  if (st) return st;
+  st = check_rows(ctx, "logits", logits, logits_type, n_keep, ld_logits);
+  if (!st) st = check_rows(ctx, "out", out, out_type, n_keep, ld_out);
+  if (st) return st;
+  if (n_keep > sph::sample_max_n()) return fail(ctx, SPH_ERR_UNSUPPORTED, "n_keep above %d", sph::sample_max_n());
+  if (sph::shape_blocks(rows, (int)n_keep, ctx->sm_count) > INT32_MAX)
+    return fail(ctx, SPH_ERR_UNSUPPORTED, "rows*n_keep too large");
+  sph::Shape a{};
+  if (shaping) {
+    const sph_shaping& s = *shaping;
+    if (s.history) {
+      if (s.max_tokens < 0 || s.max_tokens > (1 << 30) || s.ld_history < s.max_tokens)
+        return fail(ctx, SPH_ERR_INVALID_ARG, "max_tokens=%lld out of [0, 2^30] or above its row stride %lld",
+                    (long long)s.max_tokens, (long long)s.ld_history);
+    } else if (s.lengths || s.prompt_lengths || s.repetition || s.frequency || s.presence) {
+      return fail(ctx, SPH_ERR_INVALID_ARG, "penalties need history");
+    }
+    if (s.n_bias < 0 || s.n_bias > (1 << 20))
+      return fail(ctx, SPH_ERR_INVALID_ARG, "n_bias=%lld out of [0, 2^20]", (long long)s.n_bias);
+    if (s.n_bias > 0 && (!s.bias_ids || !s.bias_values || s.ld_bias_ids < s.n_bias || s.ld_bias_values < s.n_bias))
+      return fail(ctx, SPH_ERR_INVALID_ARG, "biases need ids and values with row strides of at least n_bias");
+    if (s.mask) {
+      if (s.n_masks < 1 || s.ld_mask < (V + 31) / 32)
+        return fail(ctx, SPH_ERR_INVALID_ARG, "masks of %lld ids need a row stride of %lld words", (long long)V,
+                    (long long)(V + 31) / 32);
+      if (!s.mask_rows && s.n_masks < rows)
+        return fail(ctx, SPH_ERR_INVALID_ARG, "%lld masks for %lld rows", (long long)s.n_masks, (long long)rows);
+    } else if (s.mask_rows) {
+      return fail(ctx, SPH_ERR_INVALID_ARG, "mask_rows needs masks");
+    }
+    if (s.max_tokens > 0) a.history = s.history;
+    a.ld_history = s.ld_history; a.max_tokens = (int)s.max_tokens;
+    a.lengths = s.lengths; a.prompts = s.prompt_lengths;
+    a.repetition = s.repetition; a.frequency = s.frequency; a.presence = s.presence;
+    a.bias_ids = s.bias_ids; a.ld_bias_ids = s.ld_bias_ids;
+    a.bias_values = s.bias_values; a.ld_bias_values = s.ld_bias_values; a.n_bias = (int)s.n_bias;
+    a.mask = s.mask; a.ld_mask = s.ld_mask; a.n_masks = s.n_masks; a.mask_rows = s.mask_rows;
+  }
+  if (tokens) {
+    if (!valid_temperature(temperature))
+      return fail(ctx, SPH_ERR_INVALID_ARG, "temperature must be finite and >= 0");
+    if (out_type != SPH_TAB_FP32) return fail(ctx, SPH_ERR_UNSUPPORTED, "tokens are drawn from fp32 logits");
+    if (ctx->sampler == 1 && temperature > 0.f)
+      return fail(ctx, SPH_ERR_UNSUPPORTED, "SPH_OPT_SAMPLER = 1 draws no shaped logits");
+  }
+  DeviceGuard g(ctx->device);
+  if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+  st = host_check_ids(ctx, keep_ids, n_keep, V);
+  if (st) return st;
+  if (tokens) {
+    st = ensure_scratch(ctx, sph::shape_scratch_bytes(rows, (int)n_keep, ctx->sm_count));
+    if (st) return st;
+  }
+  a.z = logits; a.ld_z = ld_logits; a.rows = rows; a.n = (int)n_keep; a.V = V; a.ids = keep_ids;
+  a.out = out; a.ld_out = ld_out;
+  a.draw = tokens != nullptr; a.greedy = temperature == 0.f; a.inv_tau = stats_inv_tau(temperature);
+  a.seed = seed; a.offset = offset; a.tokens = tokens; a.status = ctx->status;
+  return launch_status(ctx, traced(ctx, SPH_PROF_ROWS, [&] {
+                         return sph::launch_shape(a, logits_type, out_type, ctx->scratch,
+                                                  ctx->sm_count, ctx->stream);
+                       }), "shaped logits launch");
 }
 
 }  // extern "C"

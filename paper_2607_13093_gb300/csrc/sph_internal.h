@@ -410,4 +410,153 @@ size_t grad_reserve_bytes(int64_t n, int64_t d, int sm_count);
 cudaError_t launch_table_grad(TableGrad a, int src_type, int out_type, void* scratch, int sm_count,
                               cudaStream_t st);
 
+// ---- layer norm (k_norm.cu) -----------------------------------------------
+struct Norm {
+  const void* x;            // [rows, d], row stride ld_x elements
+  int64_t ld_x, rows;
+  int d;
+  const void* weight;       // [d] of param_type, or nullptr
+  const void* bias;
+  int param_type;
+  float eps;
+  int centre;               // 0: the mean is not taken off
+  void* out;                // [rows, d], row stride ld_out elements of out_type
+  int out_type;
+  int64_t ld_out;
+  float* mean;              // [rows] or nullptr
+  float* rstd;
+  int param16;              // set by the launch: weight and bias start on 16 bytes
+};
+cudaError_t launch_norm(Norm a, int x_type, int sm_count, cudaStream_t st);
+
+struct NormGrad {
+  const void* dy;           // [rows, d], row stride ld_dy elements
+  int64_t ld_dy;
+  const void* x;
+  int64_t ld_x, rows;
+  int d;
+  const void* weight;       // [d] of weight_type, or nullptr
+  int weight_type;
+  const float* mean;        // [rows], or nullptr: not centred
+  const float* rstd;
+  void* dx;                 // [rows, d], row stride ld_dx elements of dx_type
+  int dx_type;
+  int64_t ld_dx;
+  void* dw;                 // [d] or nullptr
+  void* db;
+  int accumulate;           // 1: added to what dw and db hold
+  // set by the launch
+  int param16, parts;
+  float* partial;           // [parts][2][ld_partial], or nullptr
+  int64_t ld_partial;
+};
+size_t norm_grad_scratch_bytes(int64_t rows, int d, int sm_count);
+size_t norm_grad_reserve_bytes(int64_t rows, int64_t d, int sm_count);
+cudaError_t launch_norm_grad(NormGrad a, int x_type, int dy_type, int grad_type, void* scratch,
+                             int sm_count, cudaStream_t st);
+
+// ---- rows in e4m3 with block scales (k_fp8.cu) ------------------------------
+constexpr int kFp8Block = 128;           // columns of a scale, and rows where they share one
+struct Fp8Quant {
+  const void* x;            // [rows, d], row stride ld_x elements
+  int64_t ld_x, rows;
+  int d, block_rows;        // 1 or 128
+  uint8_t* codes;           // row stride ld_codes bytes
+  int64_t ld_codes;
+  float* scales;            // of block (i, b) at i * row_step + b * col_step
+  int64_t row_step, col_step;
+  int aligned, spans;       // set by the launch
+};
+cudaError_t launch_fp8_quant(Fp8Quant a, int x_type, cudaStream_t st);
+
+struct Fp8Lookup {
+  const int32_t* tokens;    // [n], or nullptr: rows 0 .. n - 1
+  int64_t n;
+  const uint8_t* codes;     // [V, d], row stride ld_codes bytes
+  int64_t ld_codes;
+  const float* scales;      // row stride ld_scales
+  int64_t ld_scales, V;
+  int d, block_rows;
+  float scale;
+  int64_t padding;          // the id that stands for a row of zeros
+  void* out;                // [n, d], row stride ld_out elements
+  int64_t ld_out;
+  unsigned* status;
+  int spans;                // set by the launch
+};
+cudaError_t launch_fp8_lookup(const Fp8Lookup& a, int out_type, cudaStream_t st);
+
+// Product with such a table (k_fp8_tc.cu).
+struct Fp8Gemm {
+  const void* x;            // [rows, d], row stride ld_x elements of x_type
+  int64_t ld_x;
+  int rows, d, x_type;
+  const uint8_t* w_codes;   // [V], row stride ld_codes bytes
+  int64_t ld_codes;
+  const float* w_scales;    // row stride ld_scales
+  int64_t ld_scales;
+  int block_rows;
+  int64_t V;
+  const float* bias;        // [V] or nullptr
+  const int32_t* ids;       // [n] or nullptr (identity)
+  int n;
+  void* out;                // [rows, n], row stride ld_out elements of out_type
+  int64_t ld_out;
+  int out_type;             // TAB_FP32 or TAB_BF16
+  unsigned* status;
+};
+// What its work split depends on.
+struct Fp8Plan {
+  int64_t rows, n;
+  int d;
+  int sm_count, pair_units;     // SMs, CTA pairs that fit at once
+  int pair_mode;                // 0 never, 1 where it pays, 2 always
+  int gather;                   // kept ids are given
+};
+size_t fp8_gemm_scratch_bytes(const Fp8Plan& a);
+size_t fp8_gemm_reserve_bytes(int64_t rows, int64_t d);
+cudaError_t launch_fp8_gemm(const Fp8Gemm& g, const Fp8Plan& a, void* scratch, long long spin_limit,
+                            cudaStream_t st);
+
+// ---- logits with penalties, biases and masks (k_shape.cu) -------------------
+struct Shape {
+  const void* z;            // [rows, n], row stride ld_z elements
+  int64_t ld_z, rows;
+  int n;
+  int64_t V;
+  const int32_t* ids;       // [n] or nullptr (identity)
+  const int32_t* history;   // [rows, max_tokens], row stride ld_history, or nullptr
+  int64_t ld_history;
+  int max_tokens;
+  const int32_t* lengths;   // [rows] or nullptr: max_tokens
+  const int32_t* prompts;   // [rows] or nullptr: 0
+  const float* repetition;  // [rows] or nullptr, each
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_ids;  // [rows, n_bias], row stride ld_bias_ids
+  int64_t ld_bias_ids;
+  const float* bias_values;
+  int64_t ld_bias_values;
+  int n_bias;
+  const uint32_t* mask;     // [n_masks, ceil(V / 32)], row stride ld_mask, or nullptr
+  int64_t ld_mask, n_masks;
+  const int32_t* mask_rows; // [rows] or nullptr: the row's own
+  void* out;                // [rows, n], row stride ld_out elements
+  int64_t ld_out;
+  int draw, greedy;
+  float inv_tau;
+  uint64_t seed, offset;
+  int32_t* tokens;          // [rows]
+  unsigned* status;
+  // set by the launch
+  int cols, chunks, vec;    // columns of a block, blocks a row, rows on 16 bytes
+  float l2t;
+  float4* stats;            // [rows][chunks]
+};
+size_t shape_scratch_bytes(int64_t rows, int n, int sm_count);
+size_t shape_reserve_bytes(int64_t rows, int64_t n);
+int64_t shape_blocks(int64_t rows, int n, int sm_count);
+cudaError_t launch_shape(Shape a, int z_type, int out_type, void* scratch, int sm_count,
+                         cudaStream_t st);
+
 }  // namespace sph

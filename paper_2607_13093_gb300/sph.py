@@ -52,7 +52,7 @@ _sz = ctypes.c_size_t
 
 PROF_CLASSES = 8
 PROF_NAMES = ("cloud_gemm", "quantize", "local_gemm", "sample", "verify",
-              "prep", "table", "reserved7")
+              "prep", "table", "rows")
 
 
 class sph_profile(ctypes.Structure):
@@ -74,6 +74,21 @@ class sph_mx4(ctypes.Structure):
     _fields_ = [("codes", _c_void_p), ("ld_codes", _i64), ("scales", _c_void_p),
                 ("ld_scales", _i64), ("row_scale", _c_void_p), ("rows", _i64), ("d", _i64),
                 ("format", ctypes.c_int32)]
+
+
+class sph_fp8(ctypes.Structure):
+    _fields_ = [("codes", _c_void_p), ("ld_codes", _i64), ("scales", _c_void_p),
+                ("ld_scales", _i64), ("rows", _i64), ("d", _i64),
+                ("block_rows", ctypes.c_int32)]
+
+
+class sph_shaping(ctypes.Structure):
+    _fields_ = [("history", _c_void_p), ("ld_history", _i64), ("max_tokens", _i64),
+                ("lengths", _c_void_p), ("prompt_lengths", _c_void_p), ("repetition", _c_void_p),
+                ("frequency", _c_void_p), ("presence", _c_void_p), ("bias_ids", _c_void_p),
+                ("ld_bias_ids", _i64), ("bias_values", _c_void_p), ("ld_bias_values", _i64),
+                ("n_bias", _i64), ("mask", _c_void_p), ("ld_mask", _i64), ("n_masks", _i64),
+                ("mask_rows", _c_void_p)]
 
 
 # name -> (restype, argtypes), mirroring include/sph.h
@@ -127,6 +142,19 @@ _SIGNATURES = {
                              _c_void_p, _int, _i64]),
     "sph_embed_grad": (_int, [_c_void_p, _c_void_p, _i64, _c_void_p, _int, _i64, _i64, _i64, _f32,
                               _i64, _int, _c_void_p, _int, _i64]),
+    "sph_fp8_quantize": (_int, [_c_void_p, _c_void_p, _int, _i64, ctypes.POINTER(sph_fp8)]),
+    "sph_embed_fp8": (_int, [_c_void_p, _c_void_p, _i64, ctypes.POINTER(sph_fp8), _f32, _i64,
+                             _c_void_p, _int, _i64]),
+    "sph_fp8_logits": (_int, [_c_void_p, _c_void_p, _int, _i64, _i64, ctypes.POINTER(sph_fp8),
+                              _c_void_p, _c_void_p, _i64, _c_void_p, _int, _i64]),
+    "sph_layer_norm": (_int, [_c_void_p, _c_void_p, _int, _i64, _i64, _i64, _c_void_p, _c_void_p,
+                              _int, _f32, _int, _c_void_p, _int, _i64, _c_void_p, _c_void_p]),
+    "sph_layer_norm_grad": (_int, [_c_void_p, _c_void_p, _int, _i64, _c_void_p, _int, _i64, _i64,
+                                   _i64, _c_void_p, _int, _c_void_p, _c_void_p, _c_void_p, _int,
+                                   _i64, _c_void_p, _c_void_p, _int, _int]),
+    "sph_shape_logits": (_int, [_c_void_p, _c_void_p, _int, _i64, _i64, _c_void_p, _i64, _i64,
+                                ctypes.POINTER(sph_shaping), _c_void_p, _int, _i64, _f32, _u64,
+                                _u64, _c_void_p]),
 }
 
 
@@ -697,7 +725,7 @@ def sph_mx4_logits(ctx, h, W: Mx4, *, keep_ids=None, bias=None, planes=2, out=No
 
 def sph_embed(ctx, tokens, table, *, scale=1.0, padding_id=-1, out=None, dtype=None):
     """scale * table[tokens] as [T, d]: tokens int32 [T], table a tensor [V, d]
-    (bf16, fp32 or fp16) or an Mx4.  dtype: the table's own, bf16 for an Mx4.
+    (bf16, fp32 or fp16), an Mx4 or an Fp8.  dtype: the table's own, bf16 for an Mx4 or Fp8.
     Nothing is recorded for autograd: a table that requires a gradient gets it from
     sph_embed_grad."""
     r = _fast.embed(_word(ctx), tokens, table, scale, padding_id, out, dtype)
@@ -714,6 +742,13 @@ def sph_embed(ctx, tokens, table, *, scale=1.0, padding_id=-1, out=None, dtype=N
         typ, ld = _rows(out, "out", dev)
         _check(ctx, lib.sph_embed_mx4(ctx, tokens.data_ptr() if n else None, n if n else 0, c,
                                       float(scale), int(padding_id), out.data_ptr(), typ, ld))
+        return out
+    if isinstance(table, Fp8):
+        c = _fp8(table, dev)
+        out = _result(out, (n, c.d), dtype or torch.bfloat16, dev, "out")
+        typ, ld = _rows(out, "out", dev)
+        _check(ctx, lib.sph_embed_fp8(ctx, tokens.data_ptr() if n else None, n, c, float(scale),
+                                      int(padding_id), out.data_ptr(), typ, ld))
         return out
     ttyp, tld = _rows(table, "table", dev)
     V, d = table.shape
@@ -746,6 +781,271 @@ def sph_embed_grad(ctx, tokens, d_out, V: int, *, scale=1.0, padding_id=-1, accu
                                    sld, int(V), d_out.shape[1], float(scale), int(padding_id),
                                    1 if accumulate else 0, out.data_ptr(), typ, ld))
     return out
+
+
+# ---- rows in e4m3 with block scales ------------------------------------------
+
+class Fp8(NamedTuple):
+    """Rows held in e4m3 with an fp32 scale for each block of 128 columns (sph_fp8 of the
+    header): codes float8_e4m3fn (or uint8) [rows, d], row stride a multiple of 16; scales
+    fp32 [ceil(rows / block_rows), ceil(d / 128)]; block_rows 1 or 128."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    block_rows: int
+
+
+def fp8_empty(rows: int, d: int, block_rows: int = 1, device="cuda") -> Fp8:
+    """Room for `rows` rows of d columns in e4m3 blocks."""
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    if rows < 1 or d < 1:
+        raise ValueError("rows and d must be >= 1")
+    codes = torch.empty(rows, -(-d // 16) * 16, dtype=torch.float8_e4m3fn, device=device)[:, :d]
+    scales = torch.empty(-(-rows // block_rows), -(-d // 128), dtype=torch.float32, device=device)
+    return Fp8(codes, scales, block_rows)
+
+
+def _fp8(w: Fp8, dev) -> sph_fp8:
+    """The C form of w, whose scales are those of its codes' rows and columns."""
+    codes, scales, block = w
+    if codes.device != dev or scales.device != dev or codes.device.type != "cuda":
+        raise ValueError(f"the e4m3 rows are on {codes.device} and {scales.device}, not on {dev}")
+    if codes.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise ValueError("codes must be float8_e4m3fn or uint8")
+    _need(scales, torch.float32, "scales")
+    if block not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    if codes.dim() != 2 or scales.dim() != 2 or (codes.stride(1) != 1 and codes.shape[1] > 1) \
+            or (scales.stride(1) != 1 and scales.shape[1] > 1):
+        raise ValueError("codes and scales must be 2-D with unit inner stride")
+    rows, d = codes.shape
+    want = (-(-rows // block), -(-d // 128))
+    if tuple(scales.shape) != want:
+        raise ValueError(f"scales must have shape {want}, got {tuple(scales.shape)}")
+    # (the stride of a single row says nothing)
+    ld_codes = codes.stride(0) if rows > 1 else -(-d // 16) * 16
+    ld_scales = scales.stride(0) if want[0] > 1 else max(scales.stride(0), want[1])
+    return sph_fp8(codes.data_ptr(), ld_codes, scales.data_ptr(), ld_scales, rows, d, block)
+
+
+def sph_fp8_quantize(ctx, x, block_rows=1, *, out: Optional[Fp8] = None) -> Fp8:
+    """Rows of x [R, d] (bf16, fp32 or fp16, any row stride) in e4m3 blocks."""
+    if out is None:
+        r = _fast.fp8_quantize(_word(ctx), x, block_rows)
+        if type(r) is tuple:
+            return Fp8(*r, block_rows)
+        _refused(ctx, r)
+    typ, ld = _rows(x, "x")
+    if out is None:
+        out = fp8_empty(x.shape[0], x.shape[1], block_rows, x.device)
+    elif tuple(out.codes.shape) != tuple(x.shape) or out.block_rows != block_rows:
+        raise ValueError(f"out does not hold {tuple(x.shape)} in blocks of {block_rows} rows")
+    c = _fp8(out, x.device)
+    _check(ctx, lib.sph_fp8_quantize(ctx, x.data_ptr(), typ, ld, c))
+    return out
+
+
+def sph_fp8_dequantize(ctx, w: Fp8, *, out=None, dtype=torch.bfloat16):
+    """The values that w stands for, [rows, d]."""
+    r = _fast.fp8_dequantize(_word(ctx), w, out, dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
+    c = _fp8(w, w.codes.device)
+    out = _result(out, (c.rows, c.d), dtype, w.codes.device, "out")
+    typ, ld = _rows(out, "out", w.codes.device)
+    _check(ctx, lib.sph_embed_fp8(ctx, None, c.rows, c, 1.0, -1, out.data_ptr(), typ, ld))
+    return out
+
+
+def sph_fp8_logits(ctx, h, W: Fp8, *, keep_ids=None, bias=None, out=None, dtype=torch.float32):
+    """Logits [R, n] of hidden states h [R, d], taken to e4m3 with a scale for each 128
+    columns, over the kept rows of a table in e4m3 blocks.  fp32 or bf16."""
+    r = _fast.fp8_logits(_word(ctx), h, W, keep_ids, bias, out, dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
+    dev = h.device
+    typ, ld = _rows(h, "h")
+    c = _fp8(W, dev)
+    if h.shape[1] != c.d:
+        raise ValueError(f"h has {h.shape[1]} columns, the table {c.d}")
+    n = c.rows if keep_ids is None else keep_ids.numel()
+    _need(keep_ids, torch.int32, "keep_ids")
+    _need(bias, torch.float32, "bias")
+    _dense(dev, (keep_ids, "keep_ids", n), (bias, "bias", c.rows))
+    out = _result(out, (h.shape[0], n), dtype, dev, "out")
+    otyp, old = _rows(out, "out", dev)
+    _check(ctx, lib.sph_fp8_logits(ctx, h.data_ptr(), typ, h.shape[0], ld, c, _ptr(bias),
+                                   _ptr(keep_ids), n, out.data_ptr(), otyp, old))
+    return out
+
+
+# ---- operators on rows ---------------------------------------------------------
+
+def _vector(t, d, dev, name):
+    """Type of a vector of d parameters (or of their gradients); bf16's where there is none."""
+    if t is None:
+        return SPH_TAB_BF16
+    if not t.is_cuda or t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, not on {dev}")
+    if t.dtype not in _TAB_TYPES:
+        raise ValueError(f"{name} must be bfloat16, float32 or float16, got {t.dtype}")
+    if tuple(t.shape) != (d,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous of shape {(d,)}, got {tuple(t.shape)}")
+    return _TAB_TYPES[t.dtype]
+
+
+def _per_row(t, dtype, rows, dev, name):
+    if t is None:
+        return
+    _need(t, dtype, name)
+    if t.dim() != 1 or t.numel() != rows:
+        raise ValueError(f"{name} must have shape {(rows,)}, got {tuple(t.shape)}")
+    _dense(dev, (t, name, rows))
+
+
+def sph_layer_norm(ctx, x, weight=None, bias=None, *, eps=1e-5, centre=True, stats=False, out=None,
+                   dtype=None):
+    """Layer norm of the rows of x [R, d] (bf16, fp32 or fp16, any row stride); centre=False
+    leaves the mean in (root mean square norm).  Returns out (dtype: x's own), with stats also
+    mean (None without centring) and rstd, fp32 [R], which sph_layer_norm_grad takes.
+    Nothing is recorded for autograd."""
+    r = _fast.layer_norm(_word(ctx), x, weight, bias, eps, centre, stats, out, dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
+    typ, ld = _rows(x, "x")
+    dev, (R, d) = x.device, x.shape
+    wtyp, btyp = _vector(weight, d, dev, "weight"), _vector(bias, d, dev, "bias")
+    if weight is not None and bias is not None and wtyp != btyp:
+        raise ValueError(f"weight is {weight.dtype}, bias {bias.dtype}")
+    out = _result(out, (R, d), dtype or x.dtype, dev, "out")
+    otyp, old = _rows(out, "out", dev)
+    mean = torch.empty(R, dtype=torch.float32, device=dev) if stats and centre else None
+    rstd = torch.empty(R, dtype=torch.float32, device=dev) if stats else None
+    _check(ctx, lib.sph_layer_norm(ctx, x.data_ptr(), typ, R, d, ld, _ptr(weight), _ptr(bias),
+                                   wtyp if weight is not None else btyp, float(eps),
+                                   1 if centre else 0, out.data_ptr(), otyp, old, _ptr(mean),
+                                   _ptr(rstd)))
+    return (out, mean, rstd) if stats else out
+
+
+def sph_layer_norm_grad(ctx, d_out, x, weight, mean, rstd, *, bias=True, accumulate=False, d_x=None,
+                        d_weight=None, d_bias=None, dtype=None, grad_dtype=torch.float32):
+    """Gradients of sph_layer_norm from d_out [R, d]: (d_x, d_weight, d_bias).  mean None: not
+    centred.  d_weight is None where weight is, d_bias where `bias` is false.  dtype: d_x's,
+    d_out's own by default; accumulate adds the sums to d_weight and d_bias."""
+    r = _fast.layer_norm_grad(_word(ctx), d_out, x, weight, mean, rstd, bias, accumulate, d_x,
+                              d_weight, d_bias, dtype, grad_dtype)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
+    styp, sld = _rows(d_out, "d_out")
+    dev, (R, d) = d_out.device, d_out.shape
+    typ, ld = _rows(x, "x", dev)
+    if tuple(x.shape) != (R, d):
+        raise ValueError(f"x must have shape {(R, d)}, got {tuple(x.shape)}")
+    wtyp = _vector(weight, d, dev, "weight")
+    _per_row(mean, torch.float32, R, dev, "mean")
+    _per_row(rstd, torch.float32, R, dev, "rstd")
+    if accumulate and ((weight is not None and d_weight is None) or (bias and d_bias is None)):
+        raise ValueError("accumulate needs d_weight and d_bias")
+    d_x = _result(d_x, (R, d), dtype or d_out.dtype, dev, "d_x")
+    xtyp, xld = _rows(d_x, "d_x", dev)
+    if weight is None:
+        d_weight = None
+    elif d_weight is None:
+        d_weight = torch.empty(d, dtype=grad_dtype, device=dev)
+    if not bias:
+        d_bias = None
+    elif d_bias is None:
+        d_bias = torch.empty(d, dtype=d_weight.dtype if d_weight is not None else grad_dtype,
+                             device=dev)
+    gw, gb = _vector(d_weight, d, dev, "d_weight"), _vector(d_bias, d, dev, "d_bias")
+    if d_weight is not None and d_bias is not None and gw != gb:
+        raise ValueError(f"d_weight is {d_weight.dtype}, d_bias {d_bias.dtype}")
+    _check(ctx, lib.sph_layer_norm_grad(ctx, d_out.data_ptr(), styp, sld, x.data_ptr(), typ, R, d, ld,
+                                        _ptr(weight), wtyp, _ptr(mean), _ptr(rstd), d_x.data_ptr(),
+                                        xtyp, xld, _ptr(d_weight), _ptr(d_bias),
+                                        gw if d_weight is not None else gb,
+                                        1 if accumulate else 0))
+    return d_x, d_weight, d_bias
+
+
+def _lists(t, dtype, rows, dev, name):
+    """(columns, row stride) of a 2-D operand with a list a row."""
+    _need(t, dtype, name)
+    _dense(dev, (t, name, None))
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be 2-D with unit inner stride")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name} must have {rows} rows, got {t.shape[0]}")
+    return t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def sph_shape_logits(ctx, logits, V: int, *, keep_ids=None, history=None, lengths=None,
+                     prompt_lengths=None, repetition=None, frequency=None, presence=None,
+                     bias_ids=None, bias_values=None, mask=None, mask_rows=None, temperature=None,
+                     seed=0, offset=0, out=None, dtype=None, tokens=None):
+    """Logits [R, n] over the kept ids of a vocabulary of V with penalties for repeated tokens,
+    biases and masks (sph_shaping of the header), as out (dtype: the logits' own; out may be
+    logits).  With a temperature (0: greedy) returns (out, tokens int32 [R])."""
+    r = _fast.shape_logits(_word(ctx), logits, V, keep_ids, history, lengths, prompt_lengths,
+                           repetition, frequency, presence, bias_ids, bias_values, mask, mask_rows,
+                           temperature, seed, offset, out, dtype, tokens)
+    if type(r) is not int:
+        return r
+    _refused(ctx, r)
+    typ, ld = _rows(logits, "logits")
+    dev, (R, n) = logits.device, logits.shape
+    _need(keep_ids, torch.int32, "keep_ids")
+    if (keep_ids.numel() if keep_ids is not None else int(V)) != n:
+        raise ValueError(f"logits have {n} columns, not one for each kept id")
+    _dense(dev, (keep_ids, "keep_ids", n))
+    s = sph_shaping()
+    for t, dt, name in ((lengths, torch.int32, "lengths"),
+                        (prompt_lengths, torch.int32, "prompt_lengths"),
+                        (repetition, torch.float32, "repetition"),
+                        (frequency, torch.float32, "frequency"),
+                        (presence, torch.float32, "presence"),
+                        (mask_rows, torch.int32, "mask_rows")):
+        _per_row(t, dt, R, dev, name)
+        setattr(s, name, _ptr(t))
+    if history is not None:
+        s.max_tokens, s.ld_history = _lists(history, torch.int32, R, dev, "history")
+        s.history = history.data_ptr() if s.max_tokens else None
+        if s.max_tokens == 0:
+            for name in ("lengths", "prompt_lengths", "repetition", "frequency", "presence"):
+                setattr(s, name, None)
+    if (bias_ids is None) != (bias_values is None):
+        raise ValueError("bias_ids and bias_values go together")
+    if bias_ids is not None:
+        s.n_bias, s.ld_bias_ids = _lists(bias_ids, torch.int32, R, dev, "bias_ids")
+        nv, s.ld_bias_values = _lists(bias_values, torch.float32, R, dev, "bias_values")
+        if nv != s.n_bias:
+            raise ValueError(f"{s.n_bias} bias_ids a row, {nv} bias_values")
+        s.bias_ids, s.bias_values = bias_ids.data_ptr(), bias_values.data_ptr()
+    if mask is not None:
+        words, s.ld_mask = _lists(mask, torch.int32, None, dev, "mask")
+        if words < -(-int(V) // 32):
+            raise ValueError(f"a mask of {V} ids has {-(-int(V) // 32)} words, got {words}")
+        s.mask, s.n_masks = mask.data_ptr(), mask.shape[0]
+    if temperature is None and tokens is not None:
+        raise ValueError("tokens needs a temperature")
+    out = _result(out, (R, n), dtype or logits.dtype, dev, "out")
+    otyp, old = _rows(out, "out", dev)
+    if temperature is not None:
+        if tokens is None:
+            tokens = torch.empty(R, dtype=torch.int32, device=dev)
+        _need(tokens, torch.int32, "tokens")
+        _dense(dev, (tokens, "tokens", R))
+    _check(ctx, lib.sph_shape_logits(ctx, logits.data_ptr(), typ, R, ld, _ptr(keep_ids), n, int(V), s,
+                                     out.data_ptr(), otyp, old,
+                                     float(temperature) if temperature is not None else 0.0,
+                                     int(seed) & 0xFFFFFFFFFFFFFFFF,
+                                     int(offset) & 0xFFFFFFFFFFFFFFFF, _ptr(tokens)))
+    return out if temperature is None else (out, tokens)
 
 
 class Context:
@@ -836,6 +1136,71 @@ class Context:
         _refused(self.handle, r)
         return sph_embed_grad(self.handle, tokens, d_out, V, scale=scale, padding_id=padding_id,
                               accumulate=accumulate, out=out, dtype=dtype)
+
+    def fp8_quantize(self, x, block_rows=1, *, out: Optional[Fp8] = None) -> Fp8:
+        self._follow_stream()
+        if out is None:
+            r = _fast.fp8_quantize(self._word, x, block_rows)
+            if type(r) is tuple:
+                return Fp8(*r, block_rows)
+            _refused(self.handle, r)
+        return sph_fp8_quantize(self.handle, x, block_rows, out=out)
+
+    def fp8_dequantize(self, w: Fp8, *, out=None, dtype=torch.bfloat16):
+        self._follow_stream()
+        r = _fast.fp8_dequantize(self._word, w, out, dtype)
+        if type(r) is not int:
+            return r
+        _refused(self.handle, r)
+        return sph_fp8_dequantize(self.handle, w, out=out, dtype=dtype)
+
+    def fp8_logits(self, h, W: Fp8, *, keep_ids=None, bias=None, out=None, dtype=torch.float32):
+        self._follow_stream()
+        r = _fast.fp8_logits(self._word, h, W, keep_ids, bias, out, dtype)
+        if type(r) is not int:
+            return r
+        _refused(self.handle, r)
+        return sph_fp8_logits(self.handle, h, W, keep_ids=keep_ids, bias=bias, out=out, dtype=dtype)
+
+    def layer_norm(self, x, weight=None, bias=None, *, eps=1e-5, centre=True, stats=False, out=None,
+                   dtype=None):
+        self._follow_stream()
+        r = _fast.layer_norm(self._word, x, weight, bias, eps, centre, stats, out, dtype)
+        if type(r) is not int:
+            return r
+        _refused(self.handle, r)
+        return sph_layer_norm(self.handle, x, weight, bias, eps=eps, centre=centre, stats=stats,
+                              out=out, dtype=dtype)
+
+    def layer_norm_grad(self, d_out, x, weight, mean, rstd, *, bias=True, accumulate=False, d_x=None,
+                        d_weight=None, d_bias=None, dtype=None, grad_dtype=torch.float32):
+        self._follow_stream()
+        r = _fast.layer_norm_grad(self._word, d_out, x, weight, mean, rstd, bias, accumulate, d_x,
+                                  d_weight, d_bias, dtype, grad_dtype)
+        if type(r) is not int:
+            return r
+        _refused(self.handle, r)
+        return sph_layer_norm_grad(self.handle, d_out, x, weight, mean, rstd, bias=bias,
+                                   accumulate=accumulate, d_x=d_x, d_weight=d_weight, d_bias=d_bias,
+                                   dtype=dtype, grad_dtype=grad_dtype)
+
+    def shape_logits(self, logits, V: int, *, keep_ids=None, history=None, lengths=None,
+                     prompt_lengths=None, repetition=None, frequency=None, presence=None,
+                     bias_ids=None, bias_values=None, mask=None, mask_rows=None, temperature=None,
+                     seed=0, offset=0, out=None, dtype=None, tokens=None):
+        self._follow_stream()
+        r = _fast.shape_logits(self._word, logits, V, keep_ids, history, lengths, prompt_lengths,
+                               repetition, frequency, presence, bias_ids, bias_values, mask,
+                               mask_rows, temperature, seed, offset, out, dtype, tokens)
+        if type(r) is not int:
+            return r
+        _refused(self.handle, r)
+        return sph_shape_logits(self.handle, logits, V, keep_ids=keep_ids, history=history,
+                                lengths=lengths, prompt_lengths=prompt_lengths,
+                                repetition=repetition, frequency=frequency, presence=presence,
+                                bias_ids=bias_ids, bias_values=bias_values, mask=mask,
+                                mask_rows=mask_rows, temperature=temperature, seed=seed,
+                                offset=offset, out=out, dtype=dtype, tokens=tokens)
 
     def sync(self):
         sph_sync(self.handle)
