@@ -34,6 +34,22 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
   return __float2bfloat16_rn(x);
 }
 
+// Eight fp32 values at an address on 32 bytes, one access (in two, lanes 32 bytes apart
+// touch every sector twice).
+__device__ __forceinline__ void load_v8(const float* p, float (&v)[8]) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]),
+                 "=f"(v[7])
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void store_v8(float* p, const float (&v)[8]) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]),
+               "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ bool on32(const void* p) { return ((uintptr_t)p & 31) == 0; }
+
 // Eight consecutive elements at any address, by the 16-byte words that hold them (each of
 // which holds one of the elements at least).
 template <class T>

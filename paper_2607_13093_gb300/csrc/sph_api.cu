@@ -1756,10 +1756,10 @@ sph_status sph_shape_logits(sph_ctx* ctx, const void* logits, sph_tab_type logit
   if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
   st = host_check_ids(ctx, keep_ids, n_keep, V);
   if (st) return st;
-  if (tokens) {
-    st = ensure_scratch(ctx, sph::shape_scratch_bytes(rows, (int)n_keep, ctx->sm_count));
-    if (st) return st;
-  }
+  st = ensure_scratch(ctx, sph::shape_scratch_bytes(rows, (int)n_keep, tokens != nullptr,
+                                                    (a.history ? a.max_tokens : 0) + (int64_t)a.n_bias,
+                                                    ctx->sm_count));
+  if (st) return st;
   a.z = logits; a.ld_z = ld_logits; a.rows = rows; a.n = (int)n_keep; a.V = V; a.ids = keep_ids;
   a.out = out; a.ld_out = ld_out;
   a.draw = tokens != nullptr; a.greedy = temperature == 0.f; a.inv_tau = stats_inv_tau(temperature);

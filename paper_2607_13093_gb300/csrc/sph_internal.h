@@ -549,11 +549,18 @@ struct Shape {
   int32_t* tokens;          // [rows]
   unsigned* status;
   // set by the launch
-  int cols, chunks, vec;    // columns of a block, blocks a row, rows on 16 bytes
+  int cols, chunks, vec;    // columns of a warp, warps a row, rows on 16 bytes
   float l2t;
   float4* stats;            // [rows][chunks]
+  // columns that anything sparse befalls, in ascending order: column (as bits) and logit
+  float2* pairs;            // [rows][ranges][most_marks]
+  uint32_t* marks;          // [rows][ld_marks] of each 256 columns: first pair, pairs << 16; or nullptr
+  int64_t ld_marks;
+  int ranges, most_marks;   // blocks of the sparse part a row, marks one may have
+  int wide, sparse_threads; // these blocks' columns are many; they have 1024 threads
 };
-size_t shape_scratch_bytes(int64_t rows, int n, int sm_count);
+// entries: tokens and biases that a row may have
+size_t shape_scratch_bytes(int64_t rows, int n, bool draw, int64_t entries, int sm_count);
 size_t shape_reserve_bytes(int64_t rows, int64_t n);
 int64_t shape_blocks(int64_t rows, int n, int sm_count);
 cudaError_t launch_shape(Shape a, int z_type, int out_type, void* scratch, int sm_count,

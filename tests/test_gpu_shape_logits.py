@@ -244,6 +244,28 @@ def test_long_histories_and_many_biases(ctx):
     assert same(y.cpu().numpy(), ora.shape(z, n, **a, dtype=np.float32))
 
 
+@pytest.mark.parametrize("R,n", [(2, 40000), (310, 17000), (160, 70000)])
+@pytest.mark.parametrize("off", [0, 1, 3])
+def test_marks_on_both_sides_of_a_block(ctx, R, n, off):
+    # tokens around the borders of what a block counts, rows that begin off 16 bytes
+    borders = [b for b in (16384, 32768, 65536) if b < n]
+    near = np.array([b + k for b in borders for k in range(-9, 9)] + [0, n - 1])
+    rng = np.random.default_rng(n)
+    z = np.float32(rng.standard_normal((R, n)))
+    h = near[rng.integers(0, len(near), (R, 30))]
+    zd = torch.zeros(R, n + 4, device=DEV)
+    zd[:, off:off + n] = dev(z, torch.float32)
+    out = torch.empty(R, n + 4, device=DEV)[:, off:off + n]
+    a = dict(history=h, frequency=np.full(R, 0.5, np.float32), presence=np.full(R, 8.0, np.float32))
+    y, t = call(ctx, zd[:, off:off + n], n, a, out=out, temperature=0.0)
+    ctx.sync()
+    want = z.copy()
+    for r in range(R):
+        v, c = np.unique(h[r], return_counts=True)
+        want[r, v] = want[r, v] - np.float32(0.5) * c.astype(np.float32) - np.float32(8)
+    assert same(y.cpu().numpy(), want) and t.tolist() == want.argmax(1).tolist()
+
+
 def test_strided_lists(ctx):
     R, n = 4, 600
     z, a = make(R, n, n, 2, tokens=21, biases=6)
