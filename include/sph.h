@@ -169,8 +169,10 @@ typedef enum sph_option {
                                cannot be scheduled);
                                2: never.  sph_mx4_logits too, 0: for more
                                than 96 rows in two terms or more, with kept
-                               ids in four.  sph_fp8_logits: 1 always, else
-                               never.  The results are the fp32 sums of
+                               ids in four.  sph_fp8_logits, 0: for tiles
+                               of more than 192 rows, and with block_rows 128
+                               where blocks of 256 rows pad at most a fifth.
+                               The results are the fp32 sums of
                                the same products either way.               */
   SPH_OPT_SPLIT_QUANTIZE = 10, /* sph_split_step with one payload chunk: 0
                                automatic (default: in the endpoint's epilogue

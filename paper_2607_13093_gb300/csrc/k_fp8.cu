@@ -100,6 +100,9 @@ template <class T>
 __global__ void __launch_bounds__(kRowThreads) fp8_rows_kernel(const Fp8Quant a) {
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
+  for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < a.zeros;
+       i += (int64_t)gridDim.x * kRowThreads)
+    a.zero[i] = 0;
   const int lane = threadIdx.x & 31;
   const int64_t item = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
   const int64_t row = item / a.spans;

@@ -12,75 +12,26 @@
 // memory in turn, one block each, and eight warps (four for few rows) read the one that is
 // full and add it, scaled, to sums in their registers: a multiplication and a fused
 // multiply-add a value, two values an instruction.
-#include <cuda.h>
-#include <cuda_bf16.h>
-
-#include <mutex>
-#include <type_traits>
-
-#include "fp8.cuh"
-#include "sm100_ptx.cuh"
-#include "sph_internal.h"
+#include "fp8_tc.cuh"
 
 namespace sph {
 namespace {
 
 constexpr int kM = 128;                  // table rows of a tile (of a CTA)
 constexpr int kABytes = kM * kFp8Block;
-constexpr int kThreads = 384;            // 12 warps
-constexpr int kWarpW = 0, kWarpMma = 1, kWarpX = 2, kWarpOut = 4;
+constexpr int kWarpW = 0, kWarpMma = 1, kWarpX = 2, kWarpScale = 3, kWarpOut = 4;
 constexpr int kMaxStages = 12;
-constexpr int kMaxBn = 192;              // hidden-state rows of a tile
-constexpr int kAccCols = 256;            // columns of an accumulator
-constexpr int kSxSlots = 8, kSxRow = 256;
-constexpr int kSmemMax = 227 * 1024;
+constexpr int kMaxBn = 256;              // hidden-state rows of a tile
+// A block's factors (X's scales): a slot for each block on its way.  One is written
+// again once the MMAs of `stages` blocks ago are done, which began when all warps had read the
+// accumulator two before that; so no slot that is still read is, with three more than stages.
+constexpr int kSxSlots = 16;
+static_assert(kSxSlots >= kMaxStages + 3, "slots of factors");
+constexpr int kLag = 3, kMinStages = 4;
+static_assert(kLag < kMinStages, "a block's stage is free before its factors are announced");
 constexpr int kBarBytes = 1024;
-constexpr int kExtraBytes = 1024 + kBarBytes + kSxSlots * kSxRow * 4;   // beside the stages
-constexpr uint32_t kTmemCols = 512;
-constexpr long long kDrainCycles = 1ll << 20;
-
-// ---- instructions ------------------------------------------------------------
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-  return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a);
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-// Four rows by one copy, to a pair (bar: a shared::cluster address).
-__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int x, int4 rows,
-                                            uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile::gather4"
-      ".mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
-          ptx::smem_u32(dst)),
-      "l"(map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-          ptx::smem_u32(dst)),
-      "l"(src), "r"(bytes), "r"(ptx::smem_u32(bar))
-      : "memory");
-}
-// Arrivals at a barrier of either CTA of a pair (a shared::cluster address); what they
-// announce was read from tensor memory or comes by TMA.
-__device__ __forceinline__ void arrive_at(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void expect_at(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_value(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+constexpr int kSxBytes = kSxSlots * kMaxBn * 4 + 1024;     // (groups of 32 are read whole)
+constexpr int kExtraBytes = 1024 + kBarBytes + kSxBytes;   // beside the stages
 
 struct Params {
   Fp8Gemm g;
@@ -88,6 +39,7 @@ struct Params {
   int64_t ld_xs;
   int bn, row_tiles, tiles, kt; // row tiles are the fast index of a tile
   int stages, stage_bytes;
+  int ws16;                     // rows of w_scales are on 16 bytes
   long long spin_limit;
 };
 
@@ -105,9 +57,7 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   uint64_t* empty = full + kMaxStages;
   uint64_t* acc_full = empty + kMaxStages;      // [2]
   uint64_t* acc_empty = acc_full + 2;           // [2]
-  uint64_t* sx_full = acc_empty + 2;            // [kSxSlots]
-  uint64_t* sx_empty = sx_full + kSxSlots;      // [kSxSlots]
-  uint32_t* holder = reinterpret_cast<uint32_t*>(sx_empty + kSxSlots);
+  uint32_t* holder = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* s_abort = reinterpret_cast<volatile int*>(holder + 1);
   float* sx_ring = reinterpret_cast<float*>(base + (size_t)p.stages * p.stage_bytes + kBarBytes);
   // (from lane 0, so that the compiler knows that a warp takes one branch and can
@@ -123,17 +73,13 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      // W and X codes of each CTA, scattered rows of W
-      ptx::mbar_init(&full[s], 2 * kHalves + (pieces ? 32 : 0));
+      // W and X codes of each CTA, X's scales, scattered rows of W
+      ptx::mbar_init(&full[s], 2 * kHalves + (PAIR ? 2 : 32) + (pieces ? 32 : 0));
       ptx::mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&acc_full[a], 1);
       ptx::mbar_init(&acc_empty[a], 4 * H * kHalves);
-    }
-    for (int s = 0; s < kSxSlots; ++s) {
-      ptx::mbar_init(&sx_full[s], 1);
-      ptx::mbar_init(&sx_empty[s], 4 * H);
     }
     *s_abort = 0;
     ptx::fence_mbar_init();
@@ -192,7 +138,8 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     if (++stage == p.stages) { stage = 0; phase ^= 1; }
   };
   bool ok = true;
-
+  if (warp < kWarpOut) {
+  if constexpr (NC >= 96) give_registers<Regs<PAIR>::kFew>();
   if (warp == kWarpW) {
     // ---- W codes -----------------------------------------------------------
     // Groups of 32 consecutive ids are one box.  Rows of others come as 16-byte pieces by
@@ -274,10 +221,8 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
       }
     }
   } else if (warp == kWarpX) {
-    // ---- X codes and scales ------------------------------------------------
+    // ---- X codes -------------------------------------------------------------
     ptx::griddep_wait();
-    int slot = 0;
-    uint32_t slot_phase = 0;
     for (int tile = unit; ok && tile < p.tiles; tile += units) {
       const int r0 = tile % p.row_tiles * p.bn;
       for (int k = 0; k < p.kt; ++k) {
@@ -291,14 +236,6 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
             ptx::tma_load_2d(s, &map_x, k * kFp8Block, r0, &full[stage]);
         }
         __syncwarp();
-        if (!wait(&sx_empty[slot], slot_phase ^ 1)) { ok = false; break; }
-        if (lane == 0) {
-          ptx::mbar_expect_tx(&sx_full[slot], (uint32_t)p.bn * 4);
-          bulk_load(sx_ring + slot * kSxRow, p.x_scales + (int64_t)k * p.ld_xs + r0,
-                    (uint32_t)p.bn * 4, &sx_full[slot]);
-        }
-        __syncwarp();
-        if (++slot == kSxSlots) { slot = 0; slot_phase ^= 1; }
         advance();
       }
     }
@@ -327,60 +264,110 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
         if (++acc == 2) { acc = 0; acc_phase ^= 1; }
       }
     }
-  } else if (warp >= kWarpOut && warp < kWarpOut + 4 * H) {
+  } else if (warp == kWarpScale) {
+    // ---- X's scales ----------------------------------------------------------
+    // By cp.async, which arrives by itself; not at the even CTA's barrier of a pair, so there
+    // kLag blocks are on their way before the first one has to have come.
+    ptx::griddep_wait();
+    int slot = 0, behind = 0, done = 0, total = 0;       // (pair: the block to announce, its stage)
+    auto announce = [&] {
+      if (lane == 0) arrive(&full[behind]);
+      if (++behind == p.stages) behind = 0;
+      ++done;
+    };
+    for (int tile = unit; ok && tile < p.tiles; tile += units) {
+      const float* xs = p.x_scales + tile % p.row_tiles * p.bn;
+      for (int k = 0; k < p.kt; ++k) {
+        if (!wait(&empty[stage], phase ^ 1)) { ok = false; break; }
+        for (int i = lane * 4; i < p.bn; i += 128)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                           ptx::smem_u32(sx_ring + slot * p.bn + i)),
+                       "l"(xs + (int64_t)k * p.ld_xs + i)
+                       : "memory");
+        if constexpr (PAIR) {
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          if (++total > kLag) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+            __syncwarp();
+            announce();
+          }
+        } else {
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(
+                           ptx::smem_u32(&full[stage]))
+                       : "memory");
+        }
+        advance();
+        if (++slot == kSxSlots) slot = 0;
+      }
+    }
+    if constexpr (PAIR) {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncwarp();
+      while (ok && done < total) announce();
+    }
+  }
+  } else if (warp < kWarpOut + 4 * H) {
+    if constexpr (NC >= 96) take_registers<Regs<PAIR>::kMany>();
     // ---- accumulators to sums, sums to y -------------------------------------
-    constexpr int G = NC < 32 ? NC : 32;         // columns a load
+    // A thread has a table row and NC columns.  Two groups of columns are requested together,
+    // the next two as their registers come free; the accumulator goes back to the MMAs as soon
+    // as its last columns have come, before they are added.
+    constexpr int G = NC < 32 ? NC : 32;         // columns a group
+    constexpr int NG = NC / G;
     const int quarter = warp & 3;                // (the lanes that a warp may read)
     const int col0 = (warp - kWarpOut) / 4 * NC; // the warp's first column
     ptx::griddep_wait();
     int acc = 0, slot = 0;
-    uint32_t acc_phase = 0, slot_phase = 0;
-    const int groups = max(0, min(NC / G, (p.bn - col0 + G - 1) / G));
+    uint32_t acc_phase = 0;
     for (int tile = unit; ok && tile < p.tiles; tile += units) {
       const int r0 = tile % p.row_tiles * p.bn, rows = min(p.bn, g.rows - r0);
       const int j = first_row(tile) + quarter * 32 + lane;
       const bool live = j < g.n;
-      int64_t id = !live ? -1 : gather ? g.ids[j] : j;
+      const int64_t id = !live ? -1 : gather ? g.ids[j] : j;
       const bool there = id >= 0 && id < g.V;
       const float* ws = g.w_scales + (there ? id / g.block_rows : 0) * g.ld_scales;
       const float b = there && g.bias ? g.bias[id] : 0.f;
-      float next = ws[0];
+      // (four blocks' scales at a time, four blocks ahead: one ahead, their way from the L2 took
+      // longer than a block)
+      auto scales = [&](int k) {
+        if (p.ws16 && k + 4 <= p.kt) return *reinterpret_cast<const float4*>(ws + k);
+        const int last = p.kt - 1;
+        return make_float4(ws[min(k, last)], ws[min(k + 1, last)], ws[min(k + 2, last)], ws[min(k + 3, last)]);
+      };
+      float4 four = scales(0), ahead = four;
       uint64_t sum[NC / 2];
 #pragma unroll
       for (int i = 0; i < NC / 2; ++i) sum[i] = 0;
       for (int k = 0; k < p.kt; ++k) {
-        float sw = next;
-        next = ws[min(k + 1, p.kt - 1)];
-        // A block's sum times sw stays within fp32's range for sw between 2^-100 and 2^100
-        // (it is a multiple of 2^-18 below 2^25).  Where a lane's lies outside, a factor of
-        // 2^64 goes from one scale to the other.
-        const float mag = fabsf(sw);
-        float lift = 1.f;
-        if (mag > 0x1p100f) { lift = 0x1p64f; sw *= 0x1p-64f; }
-        else if (mag < 0x1p-100f && mag > 0.f) { lift = 0x1p-64f; sw *= 0x1p64f; }
-        const bool far = __any_sync(0xFFFFFFFFu, lift != 1.f);
-        const uint64_t sw2 = pack2(sw, sw);
-        if (!wait(&sx_full[slot], slot_phase) || !wait(&acc_full[acc], acc_phase, true)) {
-          ok = false;
-          break;
+        if ((k & 3) == 0) {
+          if (k > 0) four = ahead;
+          if (k + 4 < p.kt) ahead = scales(k + 4);
         }
+        float sw = (k & 2) ? ((k & 1) ? four.w : four.z) : ((k & 1) ? four.y : four.x);
+        // Where a scale is far from 1 a factor of 2^64 goes from it to the other one.
+        float lift = 1.f;
+        const float mag = fabsf(sw);
+        if (mag > kFar) { lift = 0x1p64f; sw *= 0x1p-64f; }
+        else if (mag < kNear && mag > 0.f) { lift = 0x1p-64f; sw *= 0x1p64f; }
+        const bool far = __any_sync(0xFFFFFFFFu, lift != 1.f);
+        if (!wait(&acc_full[acc], acc_phase, true)) { ok = false; break; }
         ptx::tc_fence_after();
         const uint32_t t = tmem + acc * kAccCols + col0 + ((uint32_t)(quarter * 32) << 16);
-        const float* sx = sx_ring + slot * kSxRow + col0;
-#pragma unroll
-        for (int q = 0; q < NC / G; ++q) {
-          if (q >= groups) break;
-          float v[G];
-          if constexpr (G == 32) ptx::tmem_ld32(t + q * G, v);
-          else ptx::tmem_ld16(t + q * G, v);
+        uint32_t v[2][G];
+        tmem_request(t, v[0]);
+        if constexpr (NG > 1) tmem_request(t + G, v[1]);
+        const float* sx = sx_ring + slot * p.bn + col0;
+        const uint64_t sw2 = pack2(sw, sw);
+        auto add = [&](int q, uint32_t (&of)[G]) {
           if (!far) {
 #pragma unroll
             for (int i = 0; i < G / 4; ++i) {
               const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(sx + q * G + 4 * i);
               uint64_t& lo = sum[(q * G + 4 * i) / 2];
               uint64_t& hi = sum[(q * G + 4 * i) / 2 + 1];
-              lo = fma2(mul2(pack2(v[4 * i], v[4 * i + 1]), sw2), s.x, lo);
-              hi = fma2(mul2(pack2(v[4 * i + 2], v[4 * i + 3]), sw2), s.y, hi);
+              const uint64_t t0 = pack2(of[4 * i], of[4 * i + 1]), t1 = pack2(of[4 * i + 2], of[4 * i + 3]);
+              lo = fma2(mul2(t0, sw2), s.x, lo);
+              hi = fma2(mul2(t1, sw2), s.y, hi);
             }
           } else {
 #pragma unroll
@@ -389,24 +376,39 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
               const float s0 = fminf(sx[q * G + 2 * i] * lift, 3.402823466e38f);
               const float s1 = fminf(sx[q * G + 2 * i + 1] * lift, 3.402823466e38f);
               uint64_t& at = sum[(q * G + 2 * i) / 2];
-              at = fma2(mul2(pack2(v[2 * i], v[2 * i + 1]), sw2), pack2(s0, s1), at);
+              at = fma2_here(mul2(pack2(of[2 * i], of[2 * i + 1]), sw2), pack2(s0, s1), at);
             }
           }
-        }
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          arrive(&acc_empty[acc]);
-          ptx::mbar_arrive(&sx_empty[slot]);
+        };
+        auto release = [&] {
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive(&acc_empty[acc]);
+        };
+        tmem_wait();
+        if constexpr (NG <= 2) release();
+        arrived(v[0]);
+        if constexpr (NG > 1) arrived(v[1]);
+        add(0, v[0]);
+        if constexpr (NG > 2) tmem_request(t + 2 * G, v[0]);
+        if constexpr (NG > 1) add(1, v[1]);
+        if constexpr (NG > 3) tmem_request(t + 3 * G, v[1]);
+        if constexpr (NG > 2) {
+          tmem_wait();
+          release();
+          arrived(v[0]);
+          if constexpr (NG > 3) arrived(v[1]);
+          add(2, v[0]);
+          if constexpr (NG > 3) add(3, v[1]);
         }
         if (++acc == 2) { acc = 0; acc_phase ^= 1; }
-        if (++slot == kSxSlots) { slot = 0; slot_phase ^= 1; }
+        if (++slot == kSxSlots) slot = 0;
       }
       if (!ok) break;
       // (values first, then their stores in one block without conditions)
       auto store = [&](auto* y) {
 #pragma unroll
-        for (int q = 0; q < NC / G; ++q) {
+        for (int q = 0; q < NG; ++q) {
           float v[G];
 #pragma unroll
           for (int i = 0; i < G / 2; ++i) {
@@ -451,46 +453,25 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                              const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn encode_fn() {
-  static EncodeFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
-                                         &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeFn>(f);
-  });
-  return fn;
-}
-// Codes [rows][d bytes], boxes of 128 bytes by box_rows; zeros past the last column and row.
-bool code_map(CUtensorMap* m, const void* ptr, uint64_t d, uint64_t rows, uint64_t ld,
-              uint32_t box_rows) {
-  EncodeFn fn = encode_fn();
-  if (!fn) return false;
-  const cuuint64_t dims[2] = {d, rows}, strides[1] = {ld};
-  const cuuint32_t box[2] = {kFp8Block, box_rows}, es[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct Plan {
+  int rows_as_m;                // the other kernel (k_fp8_rows.cu)
   int pair, bn, row_tiles, tiles, kt, stages, stage_bytes, units;
 };
 // As many equal tiles of hidden-state rows as these need.
 Plan plan_of(const Fp8Plan& a) {
   Plan pl{};
-  pl.pair = a.pair_units > 0 && a.pair_mode == 2;
-  const int unit = pl.pair ? 32 : 16;
+  // The other kernel where its 256 rows are at most a fifth padding (single CTAs here / that
+  // kernel, us: 256 rows x 152064 ids x 7168 383 / 253, 1024 x 256000 x 4608 1636 / 965; 128 x
+  // 128256 x 4096 109 / 136, 320 x 51302 kept ids x 3584 117 / 138).  Pairs for row tiles above
+  // 192 (scales of one row, single CTAs / pairs: 256 x 152064 x 7168 404 / 330, 1024 x 256000 x
+  // 4608 1690 / 1343; tiles of 160, 320 x 51302 112 / 120).
   const int64_t count = (a.rows + kMaxBn - 1) / kMaxBn;
+  pl.rows_as_m = a.pair_units > 0 && a.block_rows == kFp8Block &&
+                 (a.pair_mode == 2 ? a.rows > 64 : a.pair_mode == 1 && 5 * a.rows >= 4 * 256 * count);
+  pl.pair = a.pair_units > 0 && (a.pair_mode == 2 || (a.pair_mode == 1 && a.rows > 192 * count));
+  const int unit = pl.pair ? 32 : 16;
   pl.bn = (int)(((a.rows + count - 1) / count + unit - 1) / unit * unit);
   pl.row_tiles = (int)((a.rows + pl.bn - 1) / pl.bn);
   const int64_t m = pl.pair ? 2 * kM : kM;
@@ -504,16 +485,18 @@ Plan plan_of(const Fp8Plan& a) {
   return pl;
 }
 
-struct Scratch {        // X
-  int64_t ld, ld_scales;
-  size_t scales, bytes;
+struct Scratch {        // X: codes, and scales [block][ld_scales], or [row][ld_scales]
+  int64_t ld, ld_scales, tiles;
+  size_t scales, far, bytes;    // (far: a word for each of the other kernel's tiles)
 };
-Scratch scratch_of(const Plan& pl, int64_t rows, int d) {
+Scratch scratch_of(const Plan& pl, int64_t rows, int64_t n, int d) {
   Scratch o{};
   o.ld = (d + 15) / 16 * 16;
-  o.ld_scales = (int64_t)pl.row_tiles * pl.bn;
+  o.ld_scales = pl.rows_as_m ? (pl.kt + 3) / 4 * 4 : (int64_t)pl.row_tiles * pl.bn;
   o.scales = up256((size_t)(rows * o.ld));
-  o.bytes = o.scales + up256((size_t)pl.kt * o.ld_scales * 4);
+  o.far = o.scales + up256((size_t)(pl.rows_as_m ? rows : pl.kt) * o.ld_scales * 4);
+  o.tiles = pl.rows_as_m ? fp8_rows_as_m_tiles(rows, n) : 0;
+  o.bytes = o.far + up256((size_t)o.tiles * 4);
   return o;
 }
 
@@ -538,24 +521,25 @@ cudaError_t launch_bn(const Maps& m, const Params& p, int units, cudaStream_t st
   if (p.bn <= 32) return launch<32, 1, PAIR>(m, p, units, st);
   if (p.bn <= 64) return launch<32, 2, PAIR>(m, p, units, st);
   if (p.bn <= 128) return launch<64, 2, PAIR>(m, p, units, st);
-  return launch<96, 2, PAIR>(m, p, units, st);
+  if (p.bn <= 192) return launch<96, 2, PAIR>(m, p, units, st);
+  return launch<128, 2, PAIR>(m, p, units, st);
 }
-
 }  // namespace
 
-size_t fp8_gemm_scratch_bytes(const Fp8Plan& a) { return scratch_of(plan_of(a), a.rows, a.d).bytes; }
+size_t fp8_gemm_scratch_bytes(const Fp8Plan& a) { return scratch_of(plan_of(a), a.rows, a.n, a.d).bytes; }
 
-// At least what any call of up to `rows` rows and d columns takes: tiles cover at most 32
-// more rows each, and one that is not the only one has at least 64.
-size_t fp8_gemm_reserve_bytes(int64_t rows, int64_t d) {
+// At least what any call of up to so many rows, kept ids and columns takes: tiles cover at
+// most 32 more rows each, and one that is not the only one has at least 64.
+size_t fp8_gemm_reserve_bytes(int64_t rows, int64_t n, int64_t d) {
   const size_t padded = 2 * (size_t)rows + 64, kt = (size_t)((d + kFp8Block - 1) / kFp8Block);
-  return up256((size_t)rows * ((size_t)(d + 15) / 16 * 16)) + up256(kt * padded * 4);
+  return up256((size_t)rows * ((size_t)(d + 15) / 16 * 16)) + up256((kt + 3) * padded * 4) +
+         up256((size_t)fp8_rows_as_m_tiles(rows, n) * 4);
 }
 
 cudaError_t launch_fp8_gemm(const Fp8Gemm& g, const Fp8Plan& a, void* scratch, long long spin_limit,
                             cudaStream_t st) {
   const Plan pl = plan_of(a);
-  const Scratch o = scratch_of(pl, g.rows, g.d);
+  const Scratch o = scratch_of(pl, g.rows, g.n, g.d);
   char* at = static_cast<char*>(scratch);
   Params p{};
   p.g = g;
@@ -564,6 +548,7 @@ cudaError_t launch_fp8_gemm(const Fp8Gemm& g, const Fp8Plan& a, void* scratch, l
   p.bn = pl.bn; p.row_tiles = pl.row_tiles; p.tiles = pl.tiles; p.kt = pl.kt;
   p.stages = pl.stages; p.stage_bytes = pl.stage_bytes;
   p.spin_limit = spin_limit;
+  p.ws16 = ((uintptr_t)g.w_scales & 15) == 0 && g.ld_scales % 4 == 0;
   Maps m;
   if (!code_map(&m.x, at, (uint64_t)g.d, (uint64_t)g.rows, (uint64_t)o.ld,
                 (uint32_t)(pl.bn / (pl.pair ? 2 : 1))) ||
@@ -577,9 +562,15 @@ cudaError_t launch_fp8_gemm(const Fp8Gemm& g, const Fp8Plan& a, void* scratch, l
   q.x = g.x; q.ld_x = g.ld_x; q.rows = g.rows; q.d = g.d; q.block_rows = 1;
   q.codes = reinterpret_cast<uint8_t*>(at); q.ld_codes = o.ld;
   q.scales = reinterpret_cast<float*>(at + o.scales);
-  q.row_step = 1; q.col_step = o.ld_scales;
+  q.row_step = pl.rows_as_m ? o.ld_scales : 1;
+  q.col_step = pl.rows_as_m ? 1 : o.ld_scales;
+  q.zero = reinterpret_cast<int*>(at + o.far);
+  q.zeros = o.tiles;
   cudaError_t e = launch_fp8_quant(q, g.x_type, st);
   if (e != cudaSuccess) return e;
+  if (pl.rows_as_m)
+    return launch_fp8_rows_as_m(g, q.codes, o.ld, p.x_scales, o.ld_scales, q.zero, a.pair_units,
+                                spin_limit, st);
   return pl.pair ? launch_bn<true>(m, p, pl.units, st) : launch_bn<false>(m, p, pl.units, st);
 }
 

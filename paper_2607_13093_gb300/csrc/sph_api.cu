@@ -763,7 +763,7 @@ sph_status sph_reserve(sph_ctx* ctx, int64_t max_rows, int64_t max_n_keep,
   if (m > need) need = m;
   const size_t t = sph::grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
   if (t > need) need = t;
-  const size_t q = sph::fp8_gemm_reserve_bytes(max_rows, max_d);
+  const size_t q = sph::fp8_gemm_reserve_bytes(max_rows, max_n_keep, max_d);
   if (q > need) need = q;
   // the operators on rows
   const size_t n = sph::norm_grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
@@ -1601,8 +1601,8 @@ sph_status sph_fp8_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type, int6
   if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
   st = host_check_ids(ctx, keep_ids, n_keep, W->rows);
   if (st) return st;
-  const sph::Fp8Plan plan{rows, n_keep, (int)W->d, ctx->sm_count, ctx->pair_units, pair_mode(ctx),
-                          keep_ids != nullptr};
+  const sph::Fp8Plan plan{rows, n_keep, (int)W->d, W->block_rows, ctx->sm_count, ctx->pair_units,
+                          pair_mode(ctx)};
   st = ensure_scratch(ctx, sph::fp8_gemm_scratch_bytes(plan));
   if (st) return st;
   sph::Fp8Gemm m{};

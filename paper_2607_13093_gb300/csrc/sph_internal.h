@@ -465,6 +465,8 @@ struct Fp8Quant {
   int64_t ld_codes;
   float* scales;            // of block (i, b) at i * row_step + b * col_step
   int64_t row_step, col_step;
+  int* zero;                // words to clear (blocks of one row only)
+  int64_t zeros;
   int aligned, spans;       // set by the launch
 };
 cudaError_t launch_fp8_quant(Fp8Quant a, int x_type, cudaStream_t st);
@@ -508,13 +510,19 @@ struct Fp8Gemm {
 // What its work split depends on.
 struct Fp8Plan {
   int64_t rows, n;
-  int d;
+  int d, block_rows;
   int sm_count, pair_units;     // SMs, CTA pairs that fit at once
   int pair_mode;                // 0 never, 1 where it pays, 2 always
-  int gather;                   // kept ids are given
 };
+// The kernel for many hidden states and scales of 128 rows, on x's codes and scales [rows][ld_xs]
+// (k_fp8_rows.cu).
+cudaError_t launch_fp8_rows_as_m(const Fp8Gemm& g, const uint8_t* x_codes, int64_t ld_x,
+                                 const float* x_scales, int64_t ld_xs, int* far, int pair_units,
+                                 long long spin_limit, cudaStream_t st);
+// Its tiles: `far` has a word for each, zero before.
+int64_t fp8_rows_as_m_tiles(int64_t rows, int64_t n);
 size_t fp8_gemm_scratch_bytes(const Fp8Plan& a);
-size_t fp8_gemm_reserve_bytes(int64_t rows, int64_t d);
+size_t fp8_gemm_reserve_bytes(int64_t rows, int64_t n, int64_t d);
 cudaError_t launch_fp8_gemm(const Fp8Gemm& g, const Fp8Plan& a, void* scratch, long long spin_limit,
                             cudaStream_t st);
 

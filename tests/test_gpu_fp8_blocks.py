@@ -228,7 +228,7 @@ def subset(kind, V, rng):
 @pytest.mark.parametrize("block", [1, 128])
 @pytest.mark.parametrize("rows", [2, 31, 129, 260])
 @pytest.mark.parametrize("kind", ["runs", "odd", "single", "mixed", "all"])
-@pytest.mark.parametrize("pair", [1, 2])
+@pytest.mark.parametrize("pair", [0, 1, 2])
 def test_product_of_kept_rows(sph, ctx, block, rows, kind, pair):
     V, d = 700, 200
     rng = np.random.default_rng(rows)
@@ -248,21 +248,23 @@ def test_product_of_kept_rows(sph, ctx, block, rows, kind, pair):
     c.close()
 
 
-@pytest.mark.parametrize("pair", [1, 2])
-@pytest.mark.parametrize("rows,V,d", [(16, 30000, 384), (200, 30000, 256), (500, 9000, 300)])
-def test_many_tiles(sph, ctx, pair, rows, V, d):
+@pytest.mark.parametrize("pair", [0, 1, 2])
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("rows,V,d", [(16, 30000, 384), (100, 40000, 200), (200, 30000, 256),
+                                      (500, 9000, 300)])
+def test_many_tiles(sph, ctx, pair, block, rows, V, d):
     # several tiles a CTA: every logit against the 64-bit product of what the device holds
     c = sph.Context(0)
     c.set_option(sph.SPH_OPT_TC_PAIR, pair)
-    g = torch.Generator(device=DEV).manual_seed(rows)
-    w = c.fp8_quantize(torch.randn(V, d, generator=g, device=DEV) * 0.02, 128)
+    g = torch.Generator(device=DEV).manual_seed(rows + block)
+    w = c.fp8_quantize(torch.randn(V, d, generator=g, device=DEV) * 0.02, block)
     h = torch.randn(rows, d, generator=g, device=DEV)
     y = c.fp8_logits(h, w)
     c.sync()
     hq = c.fp8_quantize(h)
-    block = lambda q: q.codes.double() * q.scales.double().repeat_interleave(128, 1)[:, :d] \
+    values = lambda q: q.codes.double() * q.scales.double().repeat_interleave(128, 1)[:, :d] \
         .repeat_interleave(q.block_rows, 0)[:q.codes.shape[0]]
-    x, t = block(hq), block(w)
+    x, t = values(hq), values(w)
     want, mag = x @ t.T, x.abs() @ t.abs().T
     off = (y.double() - want).abs()
     assert (off <= (4 * 33 * 2 + 9) * U * mag + U * want.abs()).all()
@@ -271,21 +273,23 @@ def test_many_tiles(sph, ctx, pair, rows, V, d):
 
 
 @pytest.mark.parametrize("pair", [1, 2])
-def test_scales_far_apart(sph, ctx, pair):
+@pytest.mark.parametrize("block,rows", [(1, 40), (128, 40), (128, 130)])
+def test_scales_far_apart(sph, ctx, pair, block, rows):
     # a logit is finite wherever its products' magnitudes add up within range
-    V, d, rows = 300, 260, 40
+    V, d = 1500, 260
     rng = np.random.default_rng(0)
-    table = (rng.standard_normal((V, d)) * 2.0 ** rng.integers(-116, 110, (V, 1))).astype(np.float32)
+    exps = np.repeat(rng.integers(-116, 110, -(-V // block)), block)[:V, None]
+    table = (rng.standard_normal((V, d)) * 2.0 ** exps.astype(np.float64)).astype(np.float32)
     table[7] = 0
     hid = rng.standard_normal((rows, d)).astype(np.float32)
     exps = rng.integers(-100, 100, rows)
     c = sph.Context(0)
     c.set_option(sph.SPH_OPT_TC_PAIR, pair)
-    w = c.fp8_quantize(torch.tensor(table, device=DEV))
+    w = c.fp8_quantize(torch.tensor(table, device=DEV), block)
     h = torch.tensor(hid * (2.0 ** exps.astype(np.float64))[:, None], dtype=torch.float32, device=DEV)
     y = f64(c.fp8_logits(h, w))
     c.sync()
-    want, mag = ora.product8(f64(h), ora.decode8(bytes_of(w), w.scales.cpu().numpy()))
+    want, mag = ora.product8(f64(h), ora.decode8(bytes_of(w), w.scales.cpu().numpy(), block))
     inside = mag < 2.0 ** 127
     assert inside.any() and not inside.all()
     off = np.abs(y[inside] - want[inside])
@@ -307,9 +311,10 @@ def test_nan_blocks_stay_in_their_rows_and_ids(sph, ctx):
 
 def test_a_wait_that_gives_up(sph, ctx):
     c = sph.Context(0)
-    w, table = held(ctx, 300, 200, 1, 4)
-    h = make_x(9, 200, torch.float32, 1)
-    for pair in (2, 1):
+    for pair, block, rows in ((2, 1, 9), (1, 1, 9), (0, 128, 90)):
+        w, table = held(ctx, 300, 200, block, 4)
+        h = make_x(rows, 200, torch.float32, 1)
+        ctx.sync()
         c.set_option(sph.SPH_OPT_TC_PAIR, pair)
         c.set_option(sph.SPH_OPT_SPIN_LIMIT, 1)
         c.fp8_logits(h, w)
