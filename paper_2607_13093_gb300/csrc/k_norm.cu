@@ -6,8 +6,14 @@
 // All of it is fp32, the result rounded once.  The variance is taken about the mean, from
 // the row in registers (E[x^2] - mean^2 would lose what a large mean leaves).
 //
-// Bound by memory: x is read once and y written.  A row belongs to a warp (up to 1024
-// columns) or a block, whose threads hold eight columns a piece.
+// Bound by memory: x is read once and y written.  A row belongs to a warp (up to 1024 columns)
+// or a block, whose threads hold eight columns a piece as they were read.  Of many rows a block
+// is small and its threads hold several pieces, so that many rows are on their way to an SM at
+// once and few threads wait for each other: 16384 x 5120 bf16 62 us (5.4 TB/s), fp32 97 us (6.9
+// TB/s).  320 threads a row took 98 us, a ring of rows in shared memory that two groups of these
+// took in turn 171, and a branch on each type in every piece 74 (a quarter of the stalls were
+// waits for code).  Rows at any address: 16384 x 5119 bf16 101 us.  Of few rows a block has as many
+// threads as there are pieces: 500 x 4096 bf16 4.8 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -42,31 +48,51 @@ __device__ __forceinline__ float sum_row(float v, float* red) {
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
-// The weighted columns of a piece.  (A row's first piece may start before it, see below.)
-template <bool VEC>
+// The weighted columns of a piece.
+template <class T, int MODE>
 __device__ __forceinline__ void finish_piece(const Norm& a, int64_t row, int col, float mean,
-                                             float rstd, float (&v)[8]) {
-  float p[8];
+                                             float rstd, const Eight<T, MODE>& x) {
+  F2 v[4], p[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = (v[j] - mean) * rstd;
+  for (int k = 0; k < 4; ++k) v[k] = mul2(add2(x.two(k), f2(-mean)), f2(rstd));
   if (a.weight) {
-    load_param<VEC>(a.weight, a.param_type, a.param16 != 0, col, a.d, p);
+    load_param<T, MODE>(a.weight, a.param_type, col, a.d, p);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= p[j];
+    for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], p[k]);
   }
   if (a.bias) {
-    load_param<VEC>(a.bias, a.param_type, a.param16 != 0, col, a.d, p);
+    load_param<T, MODE>(a.bias, a.param_type, col, a.d, p);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += p[j];
+    for (int k = 0; k < 4; ++k) v[k] = add2(v[k], p[k]);
   }
-  store_row<true>(a.out, a.out_type, row * a.ld_out, col, a.d, v);
+  store_row<T, MODE>(a.out, a.out_type, row * a.ld_out, col, a.d, v);
+}
+template <class T, int MODE>
+__device__ __forceinline__ float sum_piece(const Eight<T, MODE>& x) {
+  return sum_of(add2(add2(x.two(0), x.two(1)), add2(x.two(2), x.two(3))));
+}
+// Squares about the mean of the piece's columns before d.
+template <class T, int MODE>
+__device__ __forceinline__ float square_piece(const Eight<T, MODE>& x, float mean, int col, int d) {
+  if (whole<MODE>(col, d)) {
+    F2 q = f2(0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const F2 v = add2(x.two(k), f2(-mean));
+      q = fma2(v, v, q);
+    }
+    return sum_of(q);
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (col + j * kStep<MODE> < d) q = __fmaf_rn(x.get(j) - mean, x.get(j) - mean, q);
+  return q;
 }
 
-// U pieces a thread.  VEC: rows of x and out are on 16 bytes.  Other rows: the first piece
-// ends at the output row's first 16-byte boundary, so that the others are stored in 16-byte
-// words.
-template <class T, int U, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 128 : U == 1 ? 1024 : kMaxThreads) norm_kernel(const Norm a) {
+// U pieces a thread.
+template <class T, int U, int MODE, bool WARP>
+__global__ void __launch_bounds__(WARP ? 128 : U == 1 ? 1024 : 512) norm_kernel(const Norm a) {
   __shared__ float red[2][32];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
@@ -75,36 +101,25 @@ __global__ void __launch_bounds__(WARP ? 128 : U == 1 ? 1024 : kMaxThreads) norm
   const int64_t row = WARP ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
   if (WARP && row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  int first = t * 8;
-  if constexpr (!VEC) {
-    const int size = a.out_type == TAB_FP32 ? 4 : 2;
-    const int head = (int)(-(intptr_t)((uintptr_t)a.out + row * a.ld_out * size) & 15) / size;
-    first += head ? head - 8 : 0;
-  }
-  float v[U][8];
+  Eight<T, MODE> v[U];
 #pragma unroll
-  for (int i = 0; i < U; ++i) load_cols<T, VEC>(x, first + i * threads * 8, a.d, v[i]);
+  for (int i = 0; i < U; ++i) {
+    const int col = piece_col<MODE>(i, t, threads);
+    if (col < a.d) v[i].load(x, col, a.d);
+  }
   float mean = 0.f;
   if (a.centre) {
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[i][j];
+      if (piece_col<MODE>(i, t, threads) < a.d) s += sum_piece(v[i]);
     mean = sum_row<WARP>(s, red[0]) / (float)a.d;
   }
   float q = 0.f;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const int col = first + i * threads * 8;
-    if (col >= 0 && col + 8 <= a.d) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) q = __fmaf_rn(v[i][j] - mean, v[i][j] - mean, q);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (col + j >= 0 && col + j < a.d) q = __fmaf_rn(v[i][j] - mean, v[i][j] - mean, q);
-    }
+    const int col = piece_col<MODE>(i, t, threads);
+    if (col < a.d) q += square_piece(v[i], mean, col, a.d);
   }
   const float rstd = 1.f / sqrtf(sum_row<WARP>(q, red[1]) / (float)a.d + a.eps);
   if (t == 0) {
@@ -113,8 +128,8 @@ __global__ void __launch_bounds__(WARP ? 128 : U == 1 ? 1024 : kMaxThreads) norm
   }
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const int col = first + i * threads * 8;
-    if (col < a.d) finish_piece<VEC>(a, row, col, mean, rstd, v[i]);
+    const int col = piece_col<MODE>(i, t, threads);
+    if (col < a.d) finish_piece(a, row, col, mean, rstd, v[i]);
   }
 }
 
@@ -126,29 +141,21 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const Norm a) {
   ptx::griddep_launch_dependents();
   const int64_t row = blockIdx.x;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  const int size = a.out_type == TAB_FP32 ? 4 : 2;
-  const int head = (int)(-(intptr_t)((uintptr_t)a.out + row * a.ld_out * size) & 15) / size;
-  const int first = (int)threadIdx.x * 8 + (head ? head - 8 : 0);
-  float mean = 0.f, v[8];
+  const int first = piece_col<0>(0, threadIdx.x, kLongThreads);
+  Eight<T, 0> v;
+  float mean = 0.f;
   if (a.centre) {
     float s = 0.f;
     for (int col = first; col < a.d; col += kLongThreads * 8) {
-      load_cols<T, false>(x, col, a.d, v);
-      float part = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) part += v[j];
-      s += part;
+      v.load(x, col, a.d);
+      s += sum_piece(v);
     }
     mean = sum_row<false>(s, red[0]) / (float)a.d;
   }
   float q = 0.f;
   for (int col = first; col < a.d; col += kLongThreads * 8) {
-    load_cols<T, false>(x, col, a.d, v);
-    float part = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (col + j >= 0 && col + j < a.d) part = __fmaf_rn(v[j] - mean, v[j] - mean, part);
-    q += part;
+    v.load(x, col, a.d);
+    q += square_piece(v, mean, col, a.d);
   }
   const float rstd = 1.f / sqrtf(sum_row<false>(q, red[1]) / (float)a.d + a.eps);
   if (threadIdx.x == 0) {
@@ -156,44 +163,50 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const Norm a) {
     if (a.rstd) a.rstd[row] = rstd;
   }
   for (int col = first; col < a.d; col += kLongThreads * 8) {
-    load_cols<T, false>(x, col, a.d, v);
-    finish_piece<false>(a, row, col, mean, rstd, v);
+    v.load(x, col, a.d);
+    finish_piece(a, row, col, mean, rstd, v);
   }
 }
 
-template <class T, bool VEC>
+template <class T, int MODE>
 cudaError_t launch_norm_v(const Norm& a, int sm_count, cudaStream_t st) {
-  // columns that the pieces of a row have to cover
-  const int cover = a.d + (VEC ? 0 : 7);
   auto warps = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)((a.rows + 3) / 4)), dim3(128), 0, st, a);
   };
   auto block = [&](auto kernel, int u) {
-    const int threads = ((cover + 8 * u - 1) / (8 * u) + 31) / 32 * 32;
+    const int threads = ((a.d + 8 * u - 1) / (8 * u) + 31) / 32 * 32;
     return launch_pdl(kernel, dim3((unsigned)a.rows), dim3(threads), 0, st, a);
   };
-  if (cover <= 32 * 8) return warps(norm_kernel<T, 1, VEC, true>);
+  if (a.d <= 32 * 8) return warps(norm_kernel<T, 1, MODE, true>);
+  // (few rows: as many threads as a row has)
   const bool few = a.rows <= 2 * (int64_t)sm_count;
-  if (!few && cover <= 32 * 16) return warps(norm_kernel<T, 2, VEC, true>);
-  if (!few && cover <= 32 * 32) return warps(norm_kernel<T, 4, VEC, true>);
-  if (few && cover <= 1024 * 8) return block(norm_kernel<T, 1, VEC, false>, 1);
-  if (cover <= kMaxThreads * 16) return block(norm_kernel<T, 2, VEC, false>, 2);
-  if (cover <= kMaxThreads * 32) return block(norm_kernel<T, 4, VEC, false>, 4);
+  if (!few && a.d <= 32 * 16) return warps(norm_kernel<T, 2, MODE, true>);
+  if (!few && a.d <= 32 * 32) return warps(norm_kernel<T, 4, MODE, true>);
+  if (few && a.d <= 1024 * 8) return block(norm_kernel<T, 1, MODE, false>, 1);
+  if (a.d <= 128 * 16) return block(norm_kernel<T, 2, MODE, false>, 2);
+  if (a.d <= 128 * 32) return block(norm_kernel<T, 4, MODE, false>, 4);
+  if (a.d <= 128 * 40) return block(norm_kernel<T, 5, MODE, false>, 5);
+  if (a.d <= kMaxThreads * 64) return block(norm_kernel<T, 8, MODE, false>, 8);
   return launch_pdl(norm_long_kernel<T>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, a);
 }
 template <class T>
-cudaError_t launch_norm_t(const Norm& a, bool vec, int sm_count, cudaStream_t st) {
-  return vec ? launch_norm_v<T, true>(a, sm_count, st) : launch_norm_v<T, false>(a, sm_count, st);
+cudaError_t launch_norm_t(const Norm& a, int mode, int sm_count, cudaStream_t st) {
+  return mode == 2   ? launch_norm_v<T, 2>(a, sm_count, st)
+         : mode == 1 ? launch_norm_v<T, 1>(a, sm_count, st)
+                     : launch_norm_v<T, 0>(a, sm_count, st);
 }
 
 }  // namespace
 
-cudaError_t launch_norm(Norm a, int x_type, int sm_count, cudaStream_t st) {
-  const bool vec = on16(a.x, a.ld_x, type_size(x_type)) && on16(a.out, a.ld_out, type_size(a.out_type));
-  a.param16 = (((uintptr_t)a.weight | (uintptr_t)a.bias) & 15) == 0;
-  if (x_type == TAB_FP32) return launch_norm_t<float>(a, vec, sm_count, st);
-  if (x_type == TAB_BF16) return launch_norm_t<__nv_bfloat16>(a, vec, sm_count, st);
-  return launch_norm_t<__half>(a, vec, sm_count, st);
+cudaError_t launch_norm(const Norm& a, int x_type, int sm_count, cudaStream_t st) {
+  const bool wide = a.d % 8 == 0 && wide_rows(a.x, a.ld_x, x_type) &&
+                    wide_rows(a.out, a.ld_out, a.out_type) && wide_rows(a.weight, 0, a.param_type) &&
+                    wide_rows(a.bias, 0, a.param_type);
+  const bool same = a.out_type == x_type && (a.param_type == x_type || (!a.weight && !a.bias));
+  const int mode = !wide ? 0 : same ? 2 : 1;
+  if (x_type == TAB_FP32) return launch_norm_t<float>(a, mode, sm_count, st);
+  if (x_type == TAB_BF16) return launch_norm_t<__nv_bfloat16>(a, mode, sm_count, st);
+  return launch_norm_t<__half>(a, mode, sm_count, st);
 }
 
 }  // namespace sph

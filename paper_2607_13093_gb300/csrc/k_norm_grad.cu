@@ -5,10 +5,15 @@
 //
 // All of it is fp32, each result rounded once.
 //
-// Bound by memory: x and dy are read once and dx written.  A row belongs to a warp (up to
-// 512 columns) or a block.  The gradients of w and b are sums over rows: each block takes
-// rows in turn and keeps the sums of its columns in registers; a second kernel adds the
-// blocks' sums in order, so equal inputs give equal bits.
+// Bound by memory: x and dy are read once and dx written.  A row belongs to a warp or a block.
+// The gradients of w and b are sums over rows: each block takes rows in turn and keeps the sums
+// of its columns in registers, and a second kernel adds the blocks' sums in order, so equal
+// inputs give equal bits.  With the sums in registers few warps find room, so the next rows
+// are on their way while one is worked on: 16-bit rows three ahead in shared memory, which each
+// thread fills and reads by itself (no barrier), fp32 rows one ahead in registers (in shared
+// memory 201 us, the two halves of a thread's 32 bytes being two requests of every sector).
+// 32768 x 4096 bf16 174 us (4.6 TB/s), fp32 16384 x 4096 142 us (5.7 TB/s).  Rows at any address
+// are read 32 columns an access, two or four bytes a lane: 32768 x 4095 bf16 327 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -21,93 +26,251 @@ namespace {
 constexpr int kMaxThreads = 512;         // of a block that holds a row
 constexpr int kLongThreads = 1024;
 
-// Sums of a row's g and g n over its threads, in one exchange.
-template <bool WARP>
-__device__ __forceinline__ float2 sum_row2(float a, float b, float2* red) {
+// Two sums over the threads of a row (a warp, or a block of at most 16 warps, or 32), in one
+// exchange: the half warps take one of them each.
+template <bool WARP, int WARPS = 16>
+__device__ __forceinline__ float2 sum_row2(float a, float b, float* red) {
+  const int lane = threadIdx.x & 31;
+  const bool upper = lane & 16;
+  float s = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-    b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
-  }
+  for (int o = 8; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
   if constexpr (!WARP) {
-    const int lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
-    if (lane == 0) red[threadIdx.x >> 5] = make_float2(a, b);
+    const int warps = (int)blockDim.x >> 5;
+    if ((lane & 15) == 0) red[(upper ? WARPS : 0) + (threadIdx.x >> 5)] = s;
     __syncthreads();
-    const float2 r = lane < warps ? red[lane] : make_float2(0.f, 0.f);
-    a = r.x;
-    b = r.y;
+    const float* mine = red + (upper ? WARPS : 0);
+    s = (lane & 15) < warps ? mine[lane & 15] : 0.f;
+    if (WARPS > 16 && (lane & 15) + 16 < warps) s += mine[(lane & 15) + 16];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-      b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
-    }
+    for (int o = 8; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
   }
-  return make_float2(a, b);
+  const float other = __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+  return upper ? make_float2(other, s) : make_float2(s, other);
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A thread's pieces of a 16-bit row on their way through its own places in shared memory, kDepth
+// rows deep, without a barrier (each thread reads what it asked for).
+constexpr int kDepth = 4;
+template <class T, int U>
+__device__ __forceinline__ void ask_row(uint32_t at, int threads, const T* row, int t, int d) {
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int col = piece_col<1>(i, t, threads);
+    if (col >= d) break;
+    cp_async16(at + (i * threads + t) * 16, row + col);
+  }
+}
+template <class T>
+__device__ __forceinline__ void take_piece(const unsigned char* at, int threads, int t, int i,
+                                           Eight<T, 1>& to) {
+  const uint4 v = reinterpret_cast<const uint4*>(at)[i * threads + t];
+  to.w[0] = v.x; to.w[1] = v.y; to.w[2] = v.z; to.w[3] = v.w;
 }
 
 // Rows first, first + step, ... of a block (or warp), which keeps the sums of its columns
-// for the weight's and the bias's gradient.  VEC: rows of x, dy and dx are on 16 bytes.
-template <class TX, class TY, int U, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 128 : kMaxThreads) norm_grad_kernel(const NormGrad a) {
-  __shared__ float2 red[2][32];
+// for the weight's and the bias's gradient.
+template <class TX, class TY, int U, int MODE, bool WARP, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGrad a) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ float red[2][32];
+  constexpr int M = MODE ? 1 : 0;
+  // 16-bit rows through shared memory; others a row ahead in registers
+  constexpr bool RING = MODE != 0 && sizeof(TX) + sizeof(TY) == 4, AHEAD = MODE != 0 && !RING;
+  // n and g of a row stay in registers over the exchange; else both are made twice (where they
+  // do not fit without spills: fp32 16384 x 4096 141 us so, 151 held)
+  constexpr bool HOLD = RING && U <= 2;
+  constexpr bool KEEP = MODE == 2 && sizeof(TX) == 2;      // the weight stays in registers
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int threads = WARP ? 32 : (int)blockDim.x;
   const int t = WARP ? threadIdx.x & 31 : threadIdx.x;
   const int owner = WARP ? (int)blockIdx.x * 4 + (threadIdx.x >> 5) : (int)blockIdx.x;
+  const int owners = WARP ? a.parts * 4 : a.parts;
   const float inv_d = 1.f / (float)a.d;
-  float sw[U][8], sb[U][8];
+  F2 sw[U][4], sb[U][4];
 #pragma unroll
   for (int i = 0; i < U; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sw[i][j] = sb[i][j] = 0.f;
-  int turn = 0;
-  for (int64_t row = owner; row < a.rows; row += a.parts, turn ^= 1) {
-    const TX* x = static_cast<const TX*>(a.x) + row * a.ld_x;
-    const TY* y = static_cast<const TY*>(a.dy) + row * a.ld_dy;
-    float n[U][8], g[U][8];
+    for (int k = 0; k < 4; ++k) sw[i][k] = sb[i][k] = f2(0.f);
+
+  Eight<TX, M> w[KEEP ? U : 1];
+  if constexpr (KEEP) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      load_cols<TX, VEC>(x, (i * threads + t) * 8, a.d, n[i]);
-      load_cols<TY, VEC>(y, (i * threads + t) * 8, a.d, g[i]);
-    }
-    const float mean = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
-    float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      float p[8];
-      const int col = (i * threads + t) * 8;
-      if (a.weight && col < a.d) load_param<VEC>(a.weight, a.weight_type, a.param16 != 0, col, a.d, p);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        n[i][j] = (n[i][j] - mean) * rstd;
-        sw[i][j] = __fmaf_rn(g[i][j], n[i][j], sw[i][j]);
-        sb[i][j] += g[i][j];
-        if (a.weight) g[i][j] *= p[j];
-        if (col + j >= a.d) g[i][j] = 0.f;      // (there p and n are not the row's)
-        s1 += g[i][j];
-        s2 = __fmaf_rn(g[i][j], n[i][j], s2);
-      }
-    }
-    const float2 s = sum_row2<WARP>(s1, s2, red[turn]);
-    const float c1 = a.mean ? s.x * inv_d : 0.f, c2 = s.y * inv_d;
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int col = (i * threads + t) * 8;
-      if (col >= a.d) break;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) g[i][j] = rstd * (g[i][j] - c1 - n[i][j] * c2);
-      store_row<VEC>(a.dx, a.dx_type, row * a.ld_dx, col, a.d, g[i]);
+      const int col = piece_col<MODE>(i, t, threads);
+      w[i].ones();
+      if (a.weight && col < a.d) w[i].load(static_cast<const TX*>(a.weight), col, a.d);
     }
   }
-  if (a.partial) {
+  auto weight = [&](int i, int col, F2 (&p)[4]) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p[k] = w[i].two(k);
+    } else if (a.weight) {
+      load_param<TX, MODE>(a.weight, a.weight_type, col, a.d, p);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p[k] = f2(1.f);
+    }
+  };
+
+  constexpr int kPlaces = U * 16;             // of a thread, for a row of x or dy
+  unsigned char* const way = smem + (WARP ? (threadIdx.x >> 5) * kDepth * 2 * kPlaces * 32 : 0);
+  auto ask = [&](int64_t row, int slot) {
+    if constexpr (RING) {
+      if (row < a.rows) {
+        const uint32_t at = ptx::smem_u32(way) + slot * 2 * kPlaces * threads;
+        ask_row<TX, U>(at, threads, static_cast<const TX*>(a.x) + row * a.ld_x, t, a.d);
+        ask_row<TY, U>(at + kPlaces * threads, threads, static_cast<const TY*>(a.dy) + row * a.ld_dy, t,
+                       a.d);
+      }
+      cp_async_commit();
+    }
+  };
+  struct Row {
+    Eight<TX, M> x[U];
+    Eight<TY, M> y[U];
+  };
+  auto read = [&](int64_t row, Row& to) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int col = piece_col<MODE>(i, t, threads);
+      if (col >= a.d) break;
+      to.x[i].load(static_cast<const TX*>(a.x) + row * a.ld_x, col, a.d);
+      to.y[i].load(static_cast<const TY*>(a.dy) + row * a.ld_dy, col, a.d);
+    }
+  };
+  // (the row's mean and rstd come one row ahead, in registers)
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto stats = [&](int64_t row) {
+    if (row < a.rows) {
+      if (a.mean) next_mean = a.mean[row];
+      next_rstd = a.rstd[row];
+    }
+  };
+  stats(owner);
+  Row next;
+  if constexpr (RING) {
+#pragma unroll
+    for (int k = 0; k < kDepth - 1; ++k) ask(owner + (int64_t)k * owners, k);
+  } else if constexpr (AHEAD) {
+    if (owner < a.rows) read(owner, next);
+  }
+
+  int turn = 0, slot = 0;
+  for (int64_t row = owner; row < a.rows; row += owners, turn ^= 1) {
+    Row now;
+    const float mean = next_mean, rstd = next_rstd;
+    if constexpr (RING) {
+      cp_async_wait<kDepth - 2>();
+      const unsigned char* at = way + slot * 2 * kPlaces * threads;
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (piece_col<MODE>(i, t, threads) >= a.d) break;
+        take_piece(at, threads, t, i, now.x[i]);
+        take_piece(at + kPlaces * threads, threads, t, i, now.y[i]);
+      }
+      ask(row + (int64_t)(kDepth - 1) * owners, slot == 0 ? kDepth - 1 : slot - 1);
+      slot = slot == kDepth - 1 ? 0 : slot + 1;
+    } else if constexpr (AHEAD) {
+      now = next;
+      if (row + owners < a.rows) read(row + owners, next);
+    } else {
+      read(row, now);
+    }
+    stats(row + owners);
+    F2 n[HOLD ? U : 1][4], g[HOLD ? U : 1][4], g1 = f2(0.f), g2 = f2(0.f);
+    const auto n_of = [&](int i, int k) { return mul2(add2(now.x[i].two(k), f2(-mean)), f2(rstd)); };
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int col = piece_col<MODE>(i, t, threads);
+      if (col >= a.d) break;
+      F2 p[4];
+      weight(i, col, p);
+      // (behind the row's end dy reads as zero, and n is -mean rstd: finite if the row's is)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const F2 dy = now.y[i].two(k), n1 = n_of(i, k), g1k = mul2(dy, p[k]);
+        sw[i][k] = fma2(dy, n1, sw[i][k]);
+        sb[i][k] = add2(sb[i][k], dy);
+        g1 = add2(g1, g1k);
+        g2 = fma2(g1k, n1, g2);
+        if constexpr (HOLD) {
+          n[i][k] = n1;
+          g[i][k] = g1k;
+        }
+      }
+    }
+    const float2 s = sum_row2<WARP>(sum_of(g1), sum_of(g2), red[turn]);
+    const F2 k1 = f2(a.mean ? -s.x * inv_d * rstd : 0.f), k2 = f2(-s.y * inv_d * rstd);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int col = piece_col<MODE>(i, t, threads);
+      if (col >= a.d) break;
+      const int at = HOLD ? i : 0;
+      if constexpr (!HOLD) {
+        F2 p[4];
+        weight(i, col, p);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          n[0][k] = n_of(i, k);
+          g[0][k] = mul2(now.y[i].two(k), p[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g[at][k] = fma2(n[at][k], k2, fma2(g[at][k], f2(rstd), k1));
+      store_row<TX, MODE>(a.dx, a.dx_type, row * a.ld_dx, col, a.d, g[at]);
+    }
+  }
+  if (!a.partial) return;
+  if constexpr (WARP) {
+    // the warps' sums of a column, added in order
+    float2* const sums = reinterpret_cast<float2*>(smem);
+    const int warp = threadIdx.x >> 5;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        sums[((warp * 2) * U * 4 + i * 4 + k) * 32 + t] = both(sw[i][k]);
+        sums[((warp * 2 + 1) * U * 4 + i * 4 + k) * 32 + t] = both(sb[i][k]);
+      }
+    __syncthreads();
+    if (warp >= 2) return;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int col = piece_col<MODE>(i, t, threads);
+      if (col >= a.d) break;
+      F2 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = f2(0.f);
+#pragma unroll
+        for (int from = 0; from < 4; ++from) {
+          const float2 q = sums[((from * 2 + warp) * U * 4 + i * 4 + k) * 32 + t];
+          v[k] = add2(v[k], f2(q.x, q.y));
+        }
+      }
+      store_eight<float, M>(a.partial, ((int64_t)blockIdx.x * 2 + warp) * a.ld_partial, col, a.d, v);
+    }
+  } else {
     float* pw = a.partial + (int64_t)owner * 2 * a.ld_partial;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int col = (i * threads + t) * 8;
+      const int col = piece_col<MODE>(i, t, threads);
       if (col >= a.d) break;
-      store_cols<float, true>(pw, col, (int)a.ld_partial, sw[i]);
-      store_cols<float, true>(pw + a.ld_partial, col, (int)a.ld_partial, sb[i]);
+      store_eight<float, M>(pw, 0, col, a.d, sw[i]);
+      store_eight<float, M>(pw, a.ld_partial, col, a.d, sb[i]);
     }
   }
 }
@@ -120,25 +283,26 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormGrad a) {
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int col = (int)blockIdx.x * 256 + lane * 8;
-  float sw[8], sb[8];
+  const int col = (int)blockIdx.x * 256 + lane;
+  F2 sw[4], sb[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) sw[j] = sb[j] = 0.f;
+  for (int k = 0; k < 4; ++k) sw[k] = sb[k] = f2(0.f);
   for (int64_t row = (int64_t)blockIdx.y * 8 + warp; row < a.rows; row += (int64_t)a.parts * 8) {
-    float n[8], g[8];
-    load_cols<TX, false>(static_cast<const TX*>(a.x) + row * a.ld_x, col, a.d, n);
-    load_cols<TY, false>(static_cast<const TY*>(a.dy) + row * a.ld_dy, col, a.d, g);
+    F2 n[4], g[4];
+    load_eight<TX, 0>(static_cast<const TX*>(a.x) + row * a.ld_x, col, a.d, n);
+    load_eight<TY, 0>(static_cast<const TY*>(a.dy) + row * a.ld_dy, col, a.d, g);
     const float mean = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sw[j] = __fmaf_rn(g[j], (n[j] - mean) * rstd, sw[j]);
-      sb[j] += g[j];
+    for (int k = 0; k < 4; ++k) {
+      sw[k] = fma2(g[k], mul2(add2(n[k], f2(-mean)), f2(rstd)), sw[k]);
+      sb[k] = add2(sb[k], g[k]);
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    part[warp][lane][j] = sw[j];
-    part[warp][lane][8 + j] = sb[j];
+  for (int k = 0; k < 4; ++k) {
+    const float2 w = both(sw[k]), b = both(sb[k]);
+    part[warp][lane][2 * k] = w.x; part[warp][lane][2 * k + 1] = w.y;
+    part[warp][lane][8 + 2 * k] = b.x; part[warp][lane][8 + 2 * k + 1] = b.y;
   }
   __syncthreads();
   const int c = (int)blockIdx.x * 256 + (int)threadIdx.x;
@@ -146,8 +310,8 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormGrad a) {
   float w = 0.f, b = 0.f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    w += part[k][threadIdx.x / 8][threadIdx.x % 8];
-    b += part[k][threadIdx.x / 8][8 + threadIdx.x % 8];
+    w += part[k][threadIdx.x % 32][threadIdx.x / 32];
+    b += part[k][threadIdx.x % 32][8 + threadIdx.x / 32];
   }
   float* p = a.partial + (int64_t)blockIdx.y * 2 * a.ld_partial;
   p[c] = w;
@@ -155,119 +319,140 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormGrad a) {
 }
 template <class TX, class TY>
 __global__ void __launch_bounds__(kLongThreads) norm_grad_long_kernel(const NormGrad a) {
-  __shared__ float2 red[32];
+  __shared__ float red[64];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int64_t row = blockIdx.x;
   const TX* x = static_cast<const TX*>(a.x) + row * a.ld_x;
   const TY* y = static_cast<const TY*>(a.dy) + row * a.ld_dy;
   const float mean = a.mean ? a.mean[row] : 0.f, rstd = a.rstd[row], inv_d = 1.f / (float)a.d;
-  float n[8], g[8], p[8], s1 = 0.f, s2 = 0.f;
+  const int first = piece_col<0>(0, threadIdx.x, kLongThreads);
+  F2 n[4], g[4], p[4];
   auto load = [&](int col) {
-    load_cols<TX, false>(x, col, a.d, n);
-    load_cols<TY, false>(y, col, a.d, g);
-    if (a.weight) load_param<false>(a.weight, a.weight_type, false, col, a.d, p);
+    load_eight<TX, 0>(x, col, a.d, n);
+    load_eight<TY, 0>(y, col, a.d, g);
+    if (a.weight) load_param<TX, 0>(a.weight, a.weight_type, col, a.d, p);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      n[j] = (n[j] - mean) * rstd;
-      if (a.weight) g[j] *= p[j];
-      if (col + j >= a.d) g[j] = 0.f;
+    for (int k = 0; k < 4; ++k) {
+      n[k] = mul2(add2(n[k], f2(-mean)), f2(rstd));
+      if (a.weight) g[k] = mul2(g[k], p[k]);
     }
   };
-  for (int col = (int)threadIdx.x * 8; col < a.d; col += kLongThreads * 8) {
+  float s1 = 0.f, s2 = 0.f;
+  for (int col = first; col < a.d; col += kLongThreads * 8) {
     load(col);
-    float t1 = 0.f, t2 = 0.f;
+    F2 t1 = f2(0.f), t2 = f2(0.f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      t1 += g[j];
-      t2 = __fmaf_rn(g[j], n[j], t2);
+    for (int k = 0; k < 4; ++k) {
+      t1 = add2(t1, g[k]);
+      t2 = fma2(g[k], n[k], t2);
     }
-    s1 += t1;
-    s2 += t2;
+    s1 += sum_of(t1);
+    s2 += sum_of(t2);
   }
-  const float2 s = sum_row2<false>(s1, s2, red);
+  const float2 s = sum_row2<false, 32>(s1, s2, red);
   const float c1 = a.mean ? s.x * inv_d : 0.f, c2 = s.y * inv_d;
-  for (int col = (int)threadIdx.x * 8; col < a.d; col += kLongThreads * 8) {
+  for (int col = first; col < a.d; col += kLongThreads * 8) {
     load(col);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = rstd * (g[j] - c1 - n[j] * c2);
-    store_row<false>(a.dx, a.dx_type, row * a.ld_dx, col, a.d, g);
+    for (int k = 0; k < 4; ++k) g[k] = mul2(f2(rstd), fma2(n[k], f2(-c2), add2(g[k], f2(-c1))));
+    store_row<TX, 0>(a.dx, a.dx_type, row * a.ld_dx, col, a.d, g);
   }
 }
 
-// The parts' sums of 32 columns, added in order, to the weight's and the bias's gradient.
-// A warp adds every eighth part.
+// The parts' sums of 32 columns of the weight's or the bias's gradient, added in order: a warp
+// adds every 16th part.
 constexpr int kJoinWarps = 16;
 template <class T>
 __global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(const NormGrad a) {
-  __shared__ float part[2][kJoinWarps][32];
+  __shared__ float part[kJoinWarps][32];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int col = (int)blockIdx.x * 32 + lane;
-  float s[2] = {0.f, 0.f};
+  void* const to = blockIdx.y ? a.db : a.dw;
+  if (!to) return;
+  float s = 0.f;
   if (col < a.d) {
-    for (int p = warp; p < a.parts; p += kJoinWarps) {
-      const float* q = a.partial + (int64_t)p * 2 * a.ld_partial + col;
-      s[0] += q[0];
-      s[1] += q[a.ld_partial];
-    }
+    const float* q = a.partial + blockIdx.y * a.ld_partial + col;
+#pragma unroll 8
+    for (int p = warp; p < a.parts; p += kJoinWarps) s += q[(int64_t)p * 2 * a.ld_partial];
   }
-  part[0][warp][lane] = s[0];
-  part[1][warp][lane] = s[1];
+  part[warp][lane] = s;
   __syncthreads();
-  void* const to = warp == 0 ? a.dw : warp == 1 ? a.db : nullptr;
-  if (!to || col >= a.d) return;
+  if (warp || col >= a.d) return;
   float v = 0.f;
 #pragma unroll
-  for (int k = 0; k < kJoinWarps; ++k) v += part[warp][k][lane];
+  for (int k = 0; k < kJoinWarps; ++k) v += part[k][lane];
   T* out = static_cast<T*>(to) + col;
   *out = from_f32<T>(a.accumulate ? to_f32(*out) + v : v);
 }
 
-// How a call's rows are divided.
+// How a call's rows are divided.  packed: x and dy have 16 bits, and a warp holds rows of up to
+// 1024 columns; ring: they come through shared memory.  Blocks of 256 threads: two an SM, whose
+// threads hold n and g (32768 x 4096 bf16 174 us; three that make both twice 196, threads of four
+// pieces 220); rows at any address three (325 us, two 383).
 struct GradPlan {
   bool warps, is_long;
-  int u, threads, parts, blocks;
+  int u, threads, parts;
 };
-GradPlan grad_plan(int64_t rows, int d, int sm_count) {
+GradPlan grad_plan(int64_t rows, int d, bool packed, bool ring, int sm_count) {
   GradPlan p{};
-  const int64_t most = (int64_t)sm_count * 4;
-  if (d <= 32 * 16) {
+  const int64_t sms = sm_count;
+  int64_t most;
+  if (d <= 32 * (packed ? 32 : 16)) {
     p.warps = true;
-    p.u = d <= 32 * 8 ? 1 : 2;
+    p.u = d <= 32 * 8 ? 1 : d <= 32 * 16 ? 2 : 4;
     p.threads = 128;
-    const int64_t blocks = (rows + 3) / 4 < 2 * most ? (rows + 3) / 4 : 2 * most;
-    p.blocks = (int)(blocks > 0 ? blocks : 1);
-    p.parts = p.blocks * 4;
+    most = sms * (!packed ? 4 : p.u == 1 ? 8 : p.u == 2 ? 4 : 3);
+    rows = (rows + 3) / 4;
   } else if (d <= kMaxThreads * 16) {
-    p.u = d <= kMaxThreads * 8 ? 1 : 2;
+    // (few rows: as many threads as a row has)
+    p.u = rows <= 2 * sms && d <= kMaxThreads * 8 ? 1 : 2;
     p.threads = ((d + 8 * p.u - 1) / (8 * p.u) + 31) / 32 * 32;
-    const int per_sm = 1024 / p.threads;
-    const int64_t units = (int64_t)sm_count * (per_sm < 1 ? 1 : per_sm > 4 ? 4 : per_sm);
-    p.blocks = p.parts = (int)(rows < units ? (rows > 0 ? rows : 1) : units);
+    const int per_sm = (packed && !ring && p.u == 2 && p.threads <= 256 ? 768 : 512) / p.threads;
+    most = sms * (per_sm < 1 ? 1 : per_sm);
   } else {
     p.is_long = true;
-    const int64_t cols = (d + 255) / 256, want = (most + cols - 1) / cols;
-    const int64_t by_rows = (rows + 7) / 8;
-    p.parts = (int)(by_rows < want ? (by_rows > 0 ? by_rows : 1) : want);
+    const int64_t cols = (d + 255) / 256;
+    most = (sms * 4 + cols - 1) / cols;
+    rows = (rows + 7) / 8;
   }
+  p.parts = (int)(rows < most ? (rows > 0 ? rows : 1) : most);
   return p;
 }
 
-template <class TX, class TY, bool VEC>
+template <class TX, class TY, int MODE>
 cudaError_t launch_grad_v(const NormGrad& a, const GradPlan& p, cudaStream_t st) {
-  const dim3 grid((unsigned)p.blocks), block((unsigned)p.threads);
+  constexpr bool packed = sizeof(TX) + sizeof(TY) == 4;
+  auto go = [&](auto kernel) {
+    const int on_way = MODE && packed ? kDepth * p.u * 32 * p.threads : 0;
+    const int sums = p.warps ? p.u * 64 * 128 : 0;
+    const int smem = on_way > sums ? on_way : sums;
+    if (smem > 40 * 1024) {         // (48 KB hold the static part too)
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e != cudaSuccess) return e;
+    }
+    return launch_pdl(kernel, dim3((unsigned)p.parts), dim3((unsigned)p.threads), smem, st, a);
+  };
+  if constexpr (packed) {
+    if (p.u == 4) return go(norm_grad_kernel<TX, TY, 4, MODE, true, 128, 3>);
+    if (p.u == 2 && !p.warps && p.threads <= 256)
+      return go(norm_grad_kernel<TX, TY, 2, MODE, false, 256, MODE ? 2 : 3>);
+  }
   if (p.warps)
-    return p.u == 1 ? launch_pdl(norm_grad_kernel<TX, TY, 1, VEC, true>, grid, block, 0, st, a)
-                    : launch_pdl(norm_grad_kernel<TX, TY, 2, VEC, true>, grid, block, 0, st, a);
-  return p.u == 1 ? launch_pdl(norm_grad_kernel<TX, TY, 1, VEC, false>, grid, block, 0, st, a)
-                  : launch_pdl(norm_grad_kernel<TX, TY, 2, VEC, false>, grid, block, 0, st, a);
+    return p.u == 1 ? go(norm_grad_kernel<TX, TY, 1, MODE, true, 128, packed ? 8 : 4>)
+                    : go(norm_grad_kernel<TX, TY, 2, MODE, true, 128, 4>);
+  return p.u == 1 ? go(norm_grad_kernel<TX, TY, 1, MODE, false, kMaxThreads, 1>)
+                  : go(norm_grad_kernel<TX, TY, 2, MODE, false, kMaxThreads, 1>);
 }
 template <class TX, class TY>
-cudaError_t launch_grad_y(const NormGrad& a, const GradPlan& p, bool vec, cudaStream_t st) {
-  if (!p.is_long)
-    return vec ? launch_grad_v<TX, TY, true>(a, p, st) : launch_grad_v<TX, TY, false>(a, p, st);
+cudaError_t launch_grad_y(const NormGrad& a, const GradPlan& p, int mode, cudaStream_t st) {
+  if (!p.is_long) {
+    if constexpr (std::is_same<TX, TY>::value)
+      if (mode == 2) return launch_grad_v<TX, TY, 2>(a, p, st);
+    return mode ? launch_grad_v<TX, TY, 1>(a, p, st) : launch_grad_v<TX, TY, 0>(a, p, st);
+  }
   if (a.partial) {
     const cudaError_t e =
         launch_pdl(norm_columns_kernel<TX, TY>, dim3((unsigned)((a.d + 255) / 256), (unsigned)p.parts),
@@ -278,44 +463,45 @@ cudaError_t launch_grad_y(const NormGrad& a, const GradPlan& p, bool vec, cudaSt
   return launch_pdl(norm_grad_long_kernel<TX, TY>, dim3((unsigned)a.rows), dim3(kLongThreads), 0, st, a);
 }
 template <class TX>
-cudaError_t launch_grad_x(const NormGrad& a, int dy_type, const GradPlan& p, bool vec, cudaStream_t st) {
-  if (dy_type == TAB_FP32) return launch_grad_y<TX, float>(a, p, vec, st);
-  if (dy_type == TAB_BF16) return launch_grad_y<TX, __nv_bfloat16>(a, p, vec, st);
-  return launch_grad_y<TX, __half>(a, p, vec, st);
+cudaError_t launch_grad_x(const NormGrad& a, int dy_type, const GradPlan& p, int mode, cudaStream_t st) {
+  if (dy_type == TAB_FP32) return launch_grad_y<TX, float>(a, p, mode, st);
+  if (dy_type == TAB_BF16) return launch_grad_y<TX, __nv_bfloat16>(a, p, mode, st);
+  return launch_grad_y<TX, __half>(a, p, mode, st);
 }
 
 int64_t partial_ld(int d) { return (d + 31) / 32 * 32; }
 
 }  // namespace
 
-size_t norm_grad_scratch_bytes(int64_t rows, int d, int sm_count) {
-  return (size_t)grad_plan(rows, d, sm_count).parts * 2 * (size_t)partial_ld(d) * 4;
+size_t norm_grad_scratch_bytes(int64_t rows, int d, int x_type, int dy_type, int sm_count) {
+  const bool packed = x_type != TAB_FP32 && dy_type != TAB_FP32;
+  return (size_t)grad_plan(rows, d, packed, false, sm_count).parts   // (a ring's are fewer)
+         * 2 * (size_t)partial_ld(d) * 4;
 }
-// At least what any call of up to `rows` rows and d columns takes: a part holds two rows of
-// sums, and there are at most 32 parts an SM of rows of 512 columns, four of longer ones.
+// At least what any call of up to `rows` rows and d columns takes: two rows of sums a part, at
+// most one part a row and twelve an SM (768 / 64 threads).
 size_t norm_grad_reserve_bytes(int64_t rows, int64_t d, int sm_count) {
-  const int64_t narrow = d < 512 ? d : 512, up = (rows + 3) / 4 * 4;
-  const size_t short_parts = (size_t)(up < (int64_t)sm_count * 32 ? up : (int64_t)sm_count * 32);
-  const size_t parts = (size_t)(rows < (int64_t)sm_count * 4 ? rows : (int64_t)sm_count * 4);
-  const size_t a = short_parts * 2 * (size_t)partial_ld((int)narrow) * 4;
-  const size_t b = (parts < 1 ? 1 : parts) * 2 * (size_t)partial_ld((int)d) * 4;
-  return a > b ? a : b;
+  const int64_t most = (int64_t)sm_count * 12, parts = rows < 1 ? 1 : rows < most ? rows : most;
+  return (size_t)parts * 2 * (size_t)partial_ld((int)d) * 4;
 }
 
 cudaError_t launch_norm_grad(NormGrad a, int x_type, int dy_type, int grad_type, void* scratch,
                              int sm_count, cudaStream_t st) {
-  const GradPlan p = grad_plan(a.rows, a.d, sm_count);
-  const bool vec = on16(a.x, a.ld_x, type_size(x_type)) && on16(a.dy, a.ld_dy, type_size(dy_type)) &&
-                   on16(a.dx, a.ld_dx, type_size(a.dx_type));
-  a.param16 = ((uintptr_t)a.weight & 15) == 0;
+  const bool wide = a.d % 8 == 0 && wide_rows(a.x, a.ld_x, x_type) &&
+                    wide_rows(a.dy, a.ld_dy, dy_type) && wide_rows(a.dx, a.ld_dx, a.dx_type) &&
+                    wide_rows(a.weight, 0, a.weight_type);
+  const bool same = dy_type == x_type && a.dx_type == x_type && (!a.weight || a.weight_type == x_type);
+  const int mode = !wide ? 0 : same ? 2 : 1;
+  const bool packed = x_type != TAB_FP32 && dy_type != TAB_FP32;
+  const GradPlan p = grad_plan(a.rows, a.d, packed, packed && mode, sm_count);
   a.parts = p.parts;
   a.ld_partial = partial_ld(a.d);
   a.partial = a.dw || a.db ? static_cast<float*>(scratch) : nullptr;
-  const cudaError_t e = x_type == TAB_FP32   ? launch_grad_x<float>(a, dy_type, p, vec, st)
-                        : x_type == TAB_BF16 ? launch_grad_x<__nv_bfloat16>(a, dy_type, p, vec, st)
-                                             : launch_grad_x<__half>(a, dy_type, p, vec, st);
+  const cudaError_t e = x_type == TAB_FP32   ? launch_grad_x<float>(a, dy_type, p, mode, st)
+                        : x_type == TAB_BF16 ? launch_grad_x<__nv_bfloat16>(a, dy_type, p, mode, st)
+                                             : launch_grad_x<__half>(a, dy_type, p, mode, st);
   if (e != cudaSuccess || !a.partial) return e;
-  const dim3 grid((unsigned)((a.d + 31) / 32)), block(kJoinWarps * 32);
+  const dim3 grid((unsigned)((a.d + 31) / 32), 2), block(kJoinWarps * 32);
   if (grad_type == TAB_FP32) return launch_pdl(norm_join_kernel<float>, grid, block, 0, st, a);
   if (grad_type == TAB_BF16) return launch_pdl(norm_join_kernel<__nv_bfloat16>, grid, block, 0, st, a);
   return launch_pdl(norm_join_kernel<__half>, grid, block, 0, st, a);

@@ -1,33 +1,168 @@
-// What the layer norm's two directions share: parameters of any type, results of any type.
+// What the layer norm's two directions share: pieces of rows, parameters and results of any type.
 #pragma once
 
+#include <type_traits>
+
 #include "rows.cuh"
+#include "sm100_ptx.cuh"
 #include "sph_internal.h"
 
 namespace sph {
 
-// Eight columns of a weight or bias row in fp32.
-template <bool VEC>
-__device__ __forceinline__ void load_param(const void* p, int type, bool on16, int col, int d,
-                                           float (&v)[8]) {
-  if (type == TAB_FP32) {
-    if (VEC && on16) load_cols<float, true>(static_cast<const float*>(p), col, d, v);
-    else load_cols<float, false>(static_cast<const float*>(p), col, d, v);
-  } else if (type == TAB_BF16) {
-    if (VEC && on16) load_cols<__nv_bfloat16, true>(static_cast<const __nv_bfloat16*>(p), col, d, v);
-    else load_cols<__nv_bfloat16, false>(static_cast<const __nv_bfloat16*>(p), col, d, v);
+// A thread holds a row in pieces of eight columns.  MODE:
+//   0  any row: the eight are 32 columns apart, a warp's accesses 32 columns side by side
+//      wherever the row starts;
+//   1  d is a multiple of 8, and all rows and parameters are on 16 bytes (fp32: 32): the eight
+//      are neighbours, read and written in one access;
+//   2  the same, and parameters and results have the type of x (and dy): no branch on a type,
+//      which in pieces unrolled five times is most of the code.
+template <int MODE>
+__device__ __forceinline__ int piece_col(int i, int t, int threads) {
+  return MODE ? (i * threads + t) * 8 : (i * threads + (t & ~31)) * 8 + (t & 31);
+}
+template <int MODE> constexpr int kStep = MODE ? 1 : 32;
+// The first and the last of the eight are before d.
+template <int MODE>
+__device__ __forceinline__ bool whole(int col, int d) { return MODE || col + 7 * 32 < d; }
+
+// Two fp32 values in one register pair: the arithmetic of both in one instruction, each result
+// rounded as the single one is.  (What these kernels issue bounds them where rows have 16 bits.)
+struct F2 {
+  unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ F2 f2(float x) { return f2(x, x); }
+__device__ __forceinline__ float2 both(F2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+  return r;
+}
+__device__ __forceinline__ float sum_of(F2 x) { const float2 r = both(x); return r.x + r.y; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
+// Eight columns as they were read: 16-bit ones stay packed.  MODE 0: those from d on read as zeros.
+template <class T, int MODE>
+struct Eight {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const T* row, int col, int d) {
+    if constexpr (MODE) {
+      const uint4 q = *reinterpret_cast<const uint4*>(row + col);
+      w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    } else {
+      const uint16_t* bits = reinterpret_cast<const uint16_t*>(row) + col;
+      uint32_t e[8];
+      if (whole<MODE>(col, d)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = bits[j * 32];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = col + j * 32 < d ? bits[j * 32] : 0u;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = e[2 * j] | e[2 * j + 1] << 16;
+    }
+  }
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (std::is_same<T, __half>::value)
+      return __half2float(__ushort_as_half((uint16_t)(j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xFFFFu)));
+    else
+      return __uint_as_float(j & 1 ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16);
+  }
+  __device__ __forceinline__ F2 two(int k) const { return f2(get(2 * k), get(2 * k + 1)); }
+  __device__ __forceinline__ void ones() {
+    const uint32_t one = std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
+    w[0] = w[1] = w[2] = w[3] = one;
+  }
+};
+template <int MODE>
+struct Eight<float, MODE> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* row, int col, int d) {
+    if constexpr (MODE) {
+      load_v8(row + col, v);
+    } else if (whole<MODE>(col, d)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = row[col + j * 32];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = col + j * 32 < d ? row[col + j * 32] : 0.f;
+    }
+  }
+  __device__ __forceinline__ float get(int j) const { return v[j]; }
+  __device__ __forceinline__ F2 two(int k) const { return f2(v[2 * k], v[2 * k + 1]); }
+};
+
+template <class T, int MODE>
+__device__ __forceinline__ void load_eight(const void* p, int col, int d, F2 (&v)[4]) {
+  Eight<T, MODE> e;
+  e.load(static_cast<const T*>(p), col, d);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = e.two(k);
+}
+template <class T, int MODE>
+__device__ __forceinline__ void store_eight(void* p, int64_t at, int col, int d, const F2 (&v2)[4]) {
+  T* row = static_cast<T*>(p) + at;
+  float v[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 r = both(v2[k]);
+    v[2 * k] = r.x; v[2 * k + 1] = r.y;
+  }
+  if constexpr (MODE == 0) {
+    if (whole<MODE>(col, d)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) row[col + j * 32] = from_f32<T>(v[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (col + j * 32 < d) row[col + j * 32] = from_f32<T>(v[j]);
+    }
+  } else if constexpr (sizeof(T) == 4) {
+    store_v8(row + col, v);
   } else {
-    if (VEC && on16) load_cols<__half, true>(static_cast<const __half*>(p), col, d, v);
-    else load_cols<__half, false>(static_cast<const __half*>(p), col, d, v);
+    store_cols<T, true>(row, col, col + 8, v);
   }
 }
-// Columns of a result row of any type (ON16: as store_cols).
-template <bool ON16>
+// Eight columns of a parameter row in fp32 (T: x's type).
+template <class T, int MODE>
+__device__ __forceinline__ void load_param(const void* p, int type, int col, int d, F2 (&v)[4]) {
+  if (MODE == 2) load_eight<T, MODE>(p, col, d, v);
+  else if (type == TAB_FP32) load_eight<float, MODE>(p, col, d, v);
+  else if (type == TAB_BF16) load_eight<__nv_bfloat16, MODE>(p, col, d, v);
+  else load_eight<__half, MODE>(p, col, d, v);
+}
+// Eight columns of a result row.
+template <class T, int MODE>
 __device__ __forceinline__ void store_row(void* p, int type, int64_t at, int col, int d,
-                                          const float (&v)[8]) {
-  if (type == TAB_FP32) store_cols<float, ON16>(static_cast<float*>(p) + at, col, d, v);
-  else if (type == TAB_BF16) store_cols<__nv_bfloat16, ON16>(static_cast<__nv_bfloat16*>(p) + at, col, d, v);
-  else store_cols<__half, ON16>(static_cast<__half*>(p) + at, col, d, v);
+                                          const F2 (&v)[4]) {
+  if (MODE == 2) store_eight<T, MODE>(p, at, col, d, v);
+  else if (type == TAB_FP32) store_eight<float, MODE>(p, at, col, d, v);
+  else if (type == TAB_BF16) store_eight<__nv_bfloat16, MODE>(p, at, col, d, v);
+  else store_eight<__half, MODE>(p, at, col, d, v);
+}
+
+// Rows of `type` can be read and written eight columns an access.
+inline bool wide_rows(const void* p, int64_t ld, int type) {
+  const int size = type_size(type);
+  return ((uintptr_t)p & (size * 8 - 1)) == 0 && (ld & 7) == 0;
 }
 
 }  // namespace sph

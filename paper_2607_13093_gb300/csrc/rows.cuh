@@ -6,6 +6,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "sph_internal.h"
 
 namespace sph {
@@ -32,6 +34,17 @@ template <> __device__ __forceinline__ float from_f32<float>(float x) { return x
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) {
   return __float2bfloat16_rn(x);
+}
+// Two values in a word, the first in the low half.
+template <class T>
+__device__ __forceinline__ uint32_t two_of(float lo, float hi) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return (uint32_t)__half_as_ushort(h.x) | (uint32_t)__half_as_ushort(h.y) << 16;
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return (uint32_t)__bfloat16_as_ushort(h.x) | (uint32_t)__bfloat16_as_ushort(h.y) << 16;
+  }
 }
 
 // Eight fp32 values at an address on 32 bytes, one access (in two, lanes 32 bytes apart
@@ -94,12 +107,17 @@ __device__ __forceinline__ void load_cols(const T* row, int col, int d, float (&
 template <class T, bool ON16>
 __device__ __forceinline__ void store_cols(T* row, int col, int d, const float (&v)[8]) {
   if (ON16 && col >= 0 && col + 8 <= d) {
-    uint4 w[sizeof(T) / 2];
-    T* e = reinterpret_cast<T*>(w);
+    uint32_t w[2 * sizeof(T)];
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = from_f32<T>(v[j]);
+      for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[j]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(row + col)[i] = w[i];
+      for (int j = 0; j < 4; ++j) w[j] = two_of<T>(v[2 * j], v[2 * j + 1]);
+    }
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+      reinterpret_cast<uint4*>(row + col)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)

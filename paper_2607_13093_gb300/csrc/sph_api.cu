@@ -1684,7 +1684,7 @@ sph_status sph_layer_norm_grad(sph_ctx* ctx, const void* d_out, sph_tab_type d_o
   DeviceGuard g(ctx->device);
   if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
   if (d_weight || d_bias) {
-    st = ensure_scratch(ctx, sph::norm_grad_scratch_bytes(rows, (int)d, ctx->sm_count));
+    st = ensure_scratch(ctx, sph::norm_grad_scratch_bytes(rows, (int)d, x_type, d_out_type, ctx->sm_count));
     if (st) return st;
   }
   sph::NormGrad a{};

@@ -425,9 +425,8 @@ struct Norm {
   int64_t ld_out;
   float* mean;              // [rows] or nullptr
   float* rstd;
-  int param16;              // set by the launch: weight and bias start on 16 bytes
 };
-cudaError_t launch_norm(Norm a, int x_type, int sm_count, cudaStream_t st);
+cudaError_t launch_norm(const Norm& a, int x_type, int sm_count, cudaStream_t st);
 
 struct NormGrad {
   const void* dy;           // [rows, d], row stride ld_dy elements
@@ -446,11 +445,11 @@ struct NormGrad {
   void* db;
   int accumulate;           // 1: added to what dw and db hold
   // set by the launch
-  int param16, parts;
+  int parts;
   float* partial;           // [parts][2][ld_partial], or nullptr
   int64_t ld_partial;
 };
-size_t norm_grad_scratch_bytes(int64_t rows, int d, int sm_count);
+size_t norm_grad_scratch_bytes(int64_t rows, int d, int x_type, int dy_type, int sm_count);
 size_t norm_grad_reserve_bytes(int64_t rows, int64_t d, int sm_count);
 cudaError_t launch_norm_grad(NormGrad a, int x_type, int dy_type, int grad_type, void* scratch,
                              int sm_count, cudaStream_t st);
