@@ -10,6 +10,7 @@
 #include <cuda_fp8.h>
 #include <stdint.h>
 
+#include "f2.cuh"
 #include "sph_internal.h"
 
 namespace sph {
@@ -38,18 +39,60 @@ __device__ __forceinline__ Fp8Scale fp8_scale(unsigned amax_bits) {
 
 // x / step, such that e4m3's rounding of it is that of the exact quotient.  The quotient by
 // the reciprocal is within an ulp or two, one correction leaves it the nearest fp32 value
-// or next to it; where that lies on a border of two codes (or on a code: its low 19 bits are
+// or next to it.  Where that lies on a border of two codes (or on a code: its low 19 bits are
 // zeros, a code's 3 bits and the border's one being above them) the remainder tells on which
-// side the exact one is, and the quotient moves one step that way.
-__device__ __forceinline__ float fp8_quotient(float x, const Fp8Scale& s) {
-  const float v = x * s.lift;
-  float q = v * s.inv;
-  q = copysignf(__fmaf_rn(__fmaf_rn(-q, s.step, v), s.inv, q), v);      // (-0 stays -0)
-  if ((__float_as_uint(q) & 0x7FFFFu) == 0 && q != 0.f) {
-    const float rest = __fmaf_rn(-q, s.step, v);          // exact
-    if (rest != 0.f) q = __int_as_float(__float_as_int(q) + ((rest > 0.f) == (q > 0.f) ? 1 : -1));
+// side the exact one is, and the quotient moves one step that way (fp8_settled).
+//
+// rest: q step - x lift, exact.  (With the remainder's sign so, -0 stays -0.)
+struct Fp8Two {
+  F2 q, rest;
+};
+__device__ __forceinline__ Fp8Two fp8_quotients(F2 x, const Fp8Scale& s) {
+  const F2 minus = mul2(x, f2(-s.lift));
+  F2 q = mul2(minus, f2(-s.inv));
+  q = fma2(fma2(q, f2(s.step), minus), f2(-s.inv), q);
+  return {q, fma2(q, f2(s.step), minus)};
+}
+__device__ __forceinline__ float fp8_settled(float q, float rest) {
+  const int bits = __float_as_int(q);
+  const int less = (bits ^ __float_as_int(rest)) >> 31 | 1;       // -1: q is too small in magnitude
+  const bool moves = ((bits & 0x7FFFF) == 0) & (rest != 0.f) & (q != 0.f);
+  return __int_as_float(moves ? bits - less : bits);
+}
+
+// The same codes for x and amax of at most 11 significant bits (bf16, fp16), by a product.  The
+// ideal quotient x 448 / amax is a border of two codes (an integer of 5 bits or fewer and a power
+// of two) or off it by 1 / (31 * 2047) at least, 2^-16.  x / scale differs from it by what
+// rounding the scale took, less than 2^-23, on the same side for the whole block: so all that lie
+// next to a border go one way, and x times the reciprocal moved by 2^-19 that way has the same
+// codes as x / scale.  Where the scale was not rounded (amax is a multiple of 7), quotients on a
+// border are exact: rounded to 18 bits they stay there, free of the product's error.  A scale of
+// 2^-126 has an exact reciprocal.  (Quotients on a border are not rare here: 1 of 400 of normal
+// bf16 values, so that most warps met some; with exact quotients and a branch for them
+// 32000 x 4096 bf16 was coded in 82 us, so in 59.)
+struct Fp8Product {
+  F2 inv, nudge;
+  bool on_border;
+};
+__device__ __forceinline__ Fp8Product fp8_product(unsigned amax_bits, const Fp8Scale& s) {
+  const float off = __fmaf_rn(s.scale, 448.f, -__uint_as_float(amax_bits));      // exact
+  const bool rounded = s.scale > 0x1p-126f && off != 0.f;
+  Fp8Product p;
+  p.on_border = s.scale > 0x1p-126f && off == 0.f;
+  p.inv = f2(s.inv * s.lift);
+  p.nudge = f2(!rounded ? 1.f : off > 0.f ? 1.f - 0x1p-19f : 1.f + 0x1p-19f);
+  return p;
+}
+// ROUND: some lane's block has quotients on a border.
+template <bool ROUND>
+__device__ __forceinline__ float2 fp8_by_product(float lo, float hi, const Fp8Product& p, F2 inv_nudged) {
+  if constexpr (!ROUND) {
+    return both(mul2(f2(lo, hi), inv_nudged));
+  } else {
+    const F2 q = mul2(f2(lo, hi), p.inv), c = mul2(q, f2(65.f));
+    const F2 high = fma2(fma2(q, f2(-1.f), c), f2(-1.f), c);             // c - (c - q): 18 bits
+    return both(mul2(high, p.nudge));
   }
-  return q;
 }
 
 // Four values to four codes, the first in the low byte (saturating at 448).

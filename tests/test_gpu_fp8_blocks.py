@@ -128,6 +128,35 @@ def test_borders_in_16_bits(sph, ctx, dtype):
         assert np.array_equal(bytes_of(w), codes)
 
 
+@pytest.mark.parametrize("dtype,bits", [(torch.bfloat16, 8), (torch.float16, 11)])
+@pytest.mark.parametrize("block", [1, 128])
+def test_every_pair_of_mantissas(sph, ctx, dtype, bits, block):
+    # quotients half way between two codes but for what rounding the scale took, and those that
+    # are exact: every significand of x under every (fp16: every 17th) significand of amax
+    half = 1 << bits - 1
+    amax = torch.arange(half, 2 * half, 1 if bits == 8 else 17, dtype=torch.float64)
+    low = 20 if bits == 8 else 3
+    x = torch.cat([torch.arange(half, 2 * half, dtype=torch.float64) * 2.0 ** -e
+                   for e in range(1, low)])
+    if block == 1:
+        x = torch.cat([x, torch.zeros(-len(x) % 127, dtype=torch.float64)]).reshape(-1, 127)
+        x[:, ::2] *= -1
+        rows = torch.cat([amax[:, None, None].expand(-1, len(x), 1),
+                          x[None].expand(len(amax), -1, -1)], 2).reshape(len(amax), -1)
+    else:
+        rows = torch.zeros(len(amax), 128 * 128, dtype=torch.float64)
+        rows[:, :len(x)] = x
+        rows[:, ::2] *= -1
+        rows[:, -1] = amax
+        rows = rows.reshape(-1, 128)
+    rows = (rows * (2.0 ** -6 if bits == 11 else 1.0)).to(dtype).to(DEV)
+    w = ctx.fp8_quantize(rows, block)
+    ctx.sync()
+    codes, scales = ora.encode8(f64(rows), block)
+    assert np.array_equal(f64(w.scales), scales.astype(np.float64))
+    assert np.array_equal(bytes_of(w), codes)
+
+
 @pytest.mark.parametrize("block", [1, 128])
 def test_quantise_extremes(sph, ctx, block):
     rng = np.random.default_rng(3)
