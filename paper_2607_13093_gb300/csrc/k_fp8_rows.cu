@@ -13,7 +13,10 @@
 // mostly): its factor is one number a block, and a value costs half an instruction.  (With
 // table rows in the lanes, as few hidden states need it, each thread reads a factor a column
 // from shared memory, which gives 128 bytes a cycle and takes twice the MMAs' time: 1024
-// rows x 256000 ids x 4608 1197 us.)
+// rows x 256000 ids x 4608 1197 us, so 953 to 1026: 2.4 PFLOP/s, where MMAs and copies alone take
+// 678.)  What is left is the additions' latency: eight warps, two a scheduler, read 128 columns
+// of an accumulator and add them (tensor pipe active 44 % of the time, issue slots 42 %); more
+// warps have too few registers for their sums (232 a thread now).
 #include "fp8_tc.cuh"
 #include "rows.cuh"
 

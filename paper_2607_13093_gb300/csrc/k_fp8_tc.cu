@@ -4,14 +4,19 @@
 //   y[r, j] = sum over blocks b of sx[r, b] * sw[id_j, b] * (qx[r, b] . qw[id_j, b])  (+ bias)
 //
 // where qx, sx are the hidden states in the same form, a scale for each row and block
-// (k_fp8.cu).  W's rows are the MMA's M = 128, the hidden states its N; a stage is one block:
-// 128 columns, a 128-byte row of codes.
+// (k_fp8.cu).  W's rows are the MMA's M = 128 (256 over a pair of CTAs), the hidden states its N;
+// a stage is one block: 128 columns, a 128-byte row of codes.
 //
 // The scales differ from block to block and are no powers of two, so a block's sums leave
 // the tensor core before they are scaled: the MMA warp fills two accumulators in tensor
 // memory in turn, one block each, and eight warps (four for few rows) read the one that is
 // full and add it, scaled, to sums in their registers: a multiplication and a fused
-// multiply-add a value, two values an instruction.
+// multiply-add a value, two values an instruction.  W's scales come four blocks ahead (one
+// block ahead the L2's latency was the block's time).
+//
+// Few rows are bound by W's codes: 8 rows x 152064 ids x 7168 169 us (6.6 TB/s), 64 x 128256 x
+// 4096 92 us (5.9 TB/s), 32 x 12000 x 3840 12.3 us; many by the additions, 1024 x 256000 x 4608
+// with scales of one row 1343 us (1.8 PFLOP/s).  Many rows and scales of 128 rows: k_fp8_rows.cu.
 #include "fp8_tc.cuh"
 
 namespace sph {
@@ -139,173 +144,173 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
   };
   bool ok = true;
   if (warp < kWarpOut) {
-  if constexpr (NC >= 96) give_registers<Regs<PAIR>::kFew>();
-  if (warp == kWarpW) {
-    // ---- W codes -----------------------------------------------------------
-    // Groups of 32 consecutive ids are one box.  Rows of others come as 16-byte pieces by
-    // cp.async, four rows an instruction, each piece where the 128-byte swizzle has it; on
-    // pairs, whose barriers wait for no generic writes (arrive_at), four rows a copy.
-    for (int tile = unit; ok && tile < p.tiles; tile += units) {
-      const int j0 = first_row(tile), last = g.n - 1;
-      int4 id = make_int4(0, 0, 0, 0);
-      unsigned solid = 0;
-      // where rows lane / 8, lane / 8 + 4, ... begin (ids outside the table, which are the
-      // caller's mistake, take a row of it)
-      const uint8_t* from[PAIR ? 1 : 32];
-      if (gather) {
-        // the ids of rows 4 lane .. 4 lane + 3, rows past the last kept id repeating it, and
-        // which 32-row groups are consecutive ids
-        const int j = j0 + 4 * lane;
-        id = make_int4(g.ids[min(j, last)], g.ids[min(j + 1, last)], g.ids[min(j + 2, last)],
-                       g.ids[min(j + 3, last)]);
-        const bool own = id.y == id.x + 1 && id.z == id.x + 2 && id.w == id.x + 3;
-        const int next = __shfl_down_sync(0xFFFFFFFFu, id.x, 1);
-        const unsigned four = __ballot_sync(0xFFFFFFFFu, own);
-        const unsigned link = __ballot_sync(0xFFFFFFFFu, next == id.w + 1);
+    if constexpr (NC >= 96) give_registers<Regs<PAIR>::kFew>();
+    if (warp == kWarpW) {
+      // ---- W codes -----------------------------------------------------------
+      // Groups of 32 consecutive ids are one box.  Rows of others come as 16-byte pieces by
+      // cp.async, four rows an instruction, each piece where the 128-byte swizzle has it; on
+      // pairs, whose barriers wait for no generic writes (arrive_at), four rows a copy.
+      for (int tile = unit; ok && tile < p.tiles; tile += units) {
+        const int j0 = first_row(tile), last = g.n - 1;
+        int4 id = make_int4(0, 0, 0, 0);
+        unsigned solid = 0;
+        // where rows lane / 8, lane / 8 + 4, ... begin (ids outside the table, which are the
+        // caller's mistake, take a row of it)
+        const uint8_t* from[PAIR ? 1 : 32];
+        if (gather) {
+          // the ids of rows 4 lane .. 4 lane + 3, rows past the last kept id repeating it, and
+          // which 32-row groups are consecutive ids
+          const int j = j0 + 4 * lane;
+          id = make_int4(g.ids[min(j, last)], g.ids[min(j + 1, last)], g.ids[min(j + 2, last)],
+                         g.ids[min(j + 3, last)]);
+          const bool own = id.y == id.x + 1 && id.z == id.x + 2 && id.w == id.x + 3;
+          const int next = __shfl_down_sync(0xFFFFFFFFu, id.x, 1);
+          const unsigned four = __ballot_sync(0xFFFFFFFFu, own);
+          const unsigned link = __ballot_sync(0xFFFFFFFFu, next == id.w + 1);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if ((four >> 8 * q & 0xFFu) == 0xFFu && (link >> 8 * q & 0x7Fu) == 0x7Fu) solid |= 1u << q;
-        if constexpr (!PAIR) {
-          if (solid != 0xFu) {
+          for (int q = 0; q < 4; ++q)
+            if ((four >> 8 * q & 0xFFu) == 0xFFu && (link >> 8 * q & 0x7Fu) == 0x7Fu) solid |= 1u << q;
+          if constexpr (!PAIR) {
+            if (solid != 0xFu) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const int row = g.ids[min(j0 + 4 * i + (lane >> 3), last)];
-              from[i] = g.w_codes + max(0, min(row, (int)g.V - 1)) * g.ld_codes;
+              for (int i = 0; i < 32; ++i) {
+                const int row = g.ids[min(j0 + 4 * i + (lane >> 3), last)];
+                from[i] = g.w_codes + max(0, min(row, (int)g.V - 1)) * g.ld_codes;
+              }
             }
           }
         }
-      }
-      for (int k = 0; k < p.kt; ++k) {
-        if (!wait(&empty[stage], phase ^ 1, true)) { ok = false; break; }
-        uint8_t* a = base + (size_t)stage * p.stage_bytes;
-        const uint32_t bar = leader(&full[stage]);
-        const int x = k * kFp8Block;
-        if (lane == 0) expect(&full[stage], pieces ? __popc(solid) * (kABytes / 4) : kABytes);
-        __syncwarp();
-        auto box = [&](uint8_t* dst, int row) {
-          if constexpr (PAIR) ptx::tma_load_2d_pair(dst, &map_w, x, row, bar);
-          else ptx::tma_load_2d(dst, &map_w, x, row, &full[stage]);
-        };
-        if (gather) {
-          if (solid >> (lane >> 3) & 1) {
-            if ((lane & 7) == 0) box(a + lane * 512, id.x);
-          } else if constexpr (PAIR) {
-            tma_gather4(a + lane * 512, &map_row, x, id, bar);
-          }
-          if constexpr (!PAIR) {
-            const int piece = lane & 7, row = lane >> 3;
-            const int at = min(x + 16 * piece, g.d - 1) & ~15;
-            const int size = max(0, min(16, g.d - (x + 16 * piece)));
-            const uint32_t even = ptx::smem_u32(a) + row * 128 + (piece ^ row) * 16;
-            const uint32_t odd = ptx::smem_u32(a) + row * 128 + (piece ^ (row + 4)) * 16;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if (solid >> q & 1) continue;
-#pragma unroll
-              for (int i = 8 * q; i < 8 * q + 8; ++i)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                 (i % 2 ? odd : even) + i * 512),
-                             "l"(from[i] + at), "r"(size)
-                             : "memory");
+        for (int k = 0; k < p.kt; ++k) {
+          if (!wait(&empty[stage], phase ^ 1, true)) { ok = false; break; }
+          uint8_t* a = base + (size_t)stage * p.stage_bytes;
+          const uint32_t bar = leader(&full[stage]);
+          const int x = k * kFp8Block;
+          if (lane == 0) expect(&full[stage], pieces ? __popc(solid) * (kABytes / 4) : kABytes);
+          __syncwarp();
+          auto box = [&](uint8_t* dst, int row) {
+            if constexpr (PAIR) ptx::tma_load_2d_pair(dst, &map_w, x, row, bar);
+            else ptx::tma_load_2d(dst, &map_w, x, row, &full[stage]);
+          };
+          if (gather) {
+            if (solid >> (lane >> 3) & 1) {
+              if ((lane & 7) == 0) box(a + lane * 512, id.x);
+            } else if constexpr (PAIR) {
+              tma_gather4(a + lane * 512, &map_row, x, id, bar);
             }
+            if constexpr (!PAIR) {
+              const int piece = lane & 7, row = lane >> 3;
+              const int at = min(x + 16 * piece, g.d - 1) & ~15;
+              const int size = max(0, min(16, g.d - (x + 16 * piece)));
+              const uint32_t even = ptx::smem_u32(a) + row * 128 + (piece ^ row) * 16;
+              const uint32_t odd = ptx::smem_u32(a) + row * 128 + (piece ^ (row + 4)) * 16;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                if (solid >> q & 1) continue;
+#pragma unroll
+                for (int i = 8 * q; i < 8 * q + 8; ++i)
+                  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                   (i % 2 ? odd : even) + i * 512),
+                               "l"(from[i] + at), "r"(size)
+                               : "memory");
+              }
+              asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(
+                               ptx::smem_u32(&full[stage]))
+                           : "memory");
+            }
+          } else if (lane == 0) {
+            // (a pair's second half may lie past the last row: any rows of the table do,
+            // for a box starts inside it)
+            box(a, min(j0, (int)g.V - 1));
+          }
+          advance();
+        }
+      }
+    } else if (warp == kWarpX) {
+      // ---- X codes -------------------------------------------------------------
+      ptx::griddep_wait();
+      for (int tile = unit; ok && tile < p.tiles; tile += units) {
+        const int r0 = tile % p.row_tiles * p.bn;
+        for (int k = 0; k < p.kt; ++k) {
+          if (!wait(&empty[stage], phase ^ 1)) { ok = false; break; }
+          if (lane == 0) {
+            uint8_t* s = base + (size_t)stage * p.stage_bytes + kABytes;
+            expect(&full[stage], (uint32_t)x_bytes);
+            if constexpr (PAIR)
+              ptx::tma_load_2d_pair(s, &map_x, k * kFp8Block, r0 + half * bnc, leader(&full[stage]));
+            else
+              ptx::tma_load_2d(s, &map_x, k * kFp8Block, r0, &full[stage]);
+          }
+          __syncwarp();
+          advance();
+        }
+      }
+    } else if (warp == kWarpMma && half == 0) {
+      // ---- MMA ---------------------------------------------------------------
+      int acc = 0;
+      uint32_t acc_phase = 0;
+      const uint32_t idesc = ptx::idesc_e4m3_f32(kHalves * kM, p.bn);
+      for (int tile = unit; ok && tile < p.tiles; tile += units) {
+        for (int k = 0; k < p.kt; ++k) {
+          if (!wait(&acc_empty[acc], acc_phase ^ 1) || !wait(&full[stage], phase)) { ok = false; break; }
+          // (what cp.async wrote is there for the MMAs' reads)
+          if (pieces) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          ptx::tc_fence_after();
+          const uint32_t s = base_addr + stage * p.stage_bytes, d = tmem + acc * kAccCols;
+          const uint32_t ad = ptx::sdesc_k128(s), bd = ptx::sdesc_k128(s + kABytes);
+          // steps of 32 columns, none past the last column
+          const int steps = min(4, (g.d - k * kFp8Block + 31) / 32);
+          for (int j = 0; j < steps; ++j) {
+            if constexpr (PAIR) ptx::umma_f8_pair(d, ad + 2 * j, bd + 2 * j, idesc, j > 0);
+            else ptx::umma_f8(d, ad + 2 * j, bd + 2 * j, idesc, j > 0);
+          }
+          commit(&empty[stage]);
+          commit(&acc_full[acc]);
+          advance();
+          if (++acc == 2) { acc = 0; acc_phase ^= 1; }
+        }
+      }
+    } else if (warp == kWarpScale) {
+      // ---- X's scales ----------------------------------------------------------
+      // By cp.async, which arrives by itself; not at the even CTA's barrier of a pair, so there
+      // kLag blocks are on their way before the first one has to have come.
+      ptx::griddep_wait();
+      int slot = 0, behind = 0, done = 0, total = 0;       // (pair: the block to announce, its stage)
+      auto announce = [&] {
+        if (lane == 0) arrive(&full[behind]);
+        if (++behind == p.stages) behind = 0;
+        ++done;
+      };
+      for (int tile = unit; ok && tile < p.tiles; tile += units) {
+        const float* xs = p.x_scales + tile % p.row_tiles * p.bn;
+        for (int k = 0; k < p.kt; ++k) {
+          if (!wait(&empty[stage], phase ^ 1)) { ok = false; break; }
+          for (int i = lane * 4; i < p.bn; i += 128)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                             ptx::smem_u32(sx_ring + slot * p.bn + i)),
+                         "l"(xs + (int64_t)k * p.ld_xs + i)
+                         : "memory");
+          if constexpr (PAIR) {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++total > kLag) {
+              asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+              __syncwarp();
+              announce();
+            }
+          } else {
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(
                              ptx::smem_u32(&full[stage]))
                          : "memory");
           }
-        } else if (lane == 0) {
-          // (a pair's second half may lie past the last row: any rows of the table do,
-          // for a box starts inside it)
-          box(a, min(j0, (int)g.V - 1));
+          advance();
+          if (++slot == kSxSlots) slot = 0;
         }
-        advance();
       }
-    }
-  } else if (warp == kWarpX) {
-    // ---- X codes -------------------------------------------------------------
-    ptx::griddep_wait();
-    for (int tile = unit; ok && tile < p.tiles; tile += units) {
-      const int r0 = tile % p.row_tiles * p.bn;
-      for (int k = 0; k < p.kt; ++k) {
-        if (!wait(&empty[stage], phase ^ 1)) { ok = false; break; }
-        if (lane == 0) {
-          uint8_t* s = base + (size_t)stage * p.stage_bytes + kABytes;
-          expect(&full[stage], (uint32_t)x_bytes);
-          if constexpr (PAIR)
-            ptx::tma_load_2d_pair(s, &map_x, k * kFp8Block, r0 + half * bnc, leader(&full[stage]));
-          else
-            ptx::tma_load_2d(s, &map_x, k * kFp8Block, r0, &full[stage]);
-        }
+      if constexpr (PAIR) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
-        advance();
+        while (ok && done < total) announce();
       }
     }
-  } else if (warp == kWarpMma && half == 0) {
-    // ---- MMA ---------------------------------------------------------------
-    int acc = 0;
-    uint32_t acc_phase = 0;
-    const uint32_t idesc = ptx::idesc_e4m3_f32(kHalves * kM, p.bn);
-    for (int tile = unit; ok && tile < p.tiles; tile += units) {
-      for (int k = 0; k < p.kt; ++k) {
-        if (!wait(&acc_empty[acc], acc_phase ^ 1) || !wait(&full[stage], phase)) { ok = false; break; }
-        // (what cp.async wrote is there for the MMAs' reads)
-        if (pieces) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        ptx::tc_fence_after();
-        const uint32_t s = base_addr + stage * p.stage_bytes, d = tmem + acc * kAccCols;
-        const uint32_t ad = ptx::sdesc_k128(s), bd = ptx::sdesc_k128(s + kABytes);
-        // steps of 32 columns, none past the last column
-        const int steps = min(4, (g.d - k * kFp8Block + 31) / 32);
-        for (int j = 0; j < steps; ++j) {
-          if constexpr (PAIR) ptx::umma_f8_pair(d, ad + 2 * j, bd + 2 * j, idesc, j > 0);
-          else ptx::umma_f8(d, ad + 2 * j, bd + 2 * j, idesc, j > 0);
-        }
-        commit(&empty[stage]);
-        commit(&acc_full[acc]);
-        advance();
-        if (++acc == 2) { acc = 0; acc_phase ^= 1; }
-      }
-    }
-  } else if (warp == kWarpScale) {
-    // ---- X's scales ----------------------------------------------------------
-    // By cp.async, which arrives by itself; not at the even CTA's barrier of a pair, so there
-    // kLag blocks are on their way before the first one has to have come.
-    ptx::griddep_wait();
-    int slot = 0, behind = 0, done = 0, total = 0;       // (pair: the block to announce, its stage)
-    auto announce = [&] {
-      if (lane == 0) arrive(&full[behind]);
-      if (++behind == p.stages) behind = 0;
-      ++done;
-    };
-    for (int tile = unit; ok && tile < p.tiles; tile += units) {
-      const float* xs = p.x_scales + tile % p.row_tiles * p.bn;
-      for (int k = 0; k < p.kt; ++k) {
-        if (!wait(&empty[stage], phase ^ 1)) { ok = false; break; }
-        for (int i = lane * 4; i < p.bn; i += 128)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
-                           ptx::smem_u32(sx_ring + slot * p.bn + i)),
-                       "l"(xs + (int64_t)k * p.ld_xs + i)
-                       : "memory");
-        if constexpr (PAIR) {
-          asm volatile("cp.async.commit_group;" ::: "memory");
-          if (++total > kLag) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-            __syncwarp();
-            announce();
-          }
-        } else {
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(
-                           ptx::smem_u32(&full[stage]))
-                       : "memory");
-        }
-        advance();
-        if (++slot == kSxSlots) slot = 0;
-      }
-    }
-    if constexpr (PAIR) {
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
-      __syncwarp();
-      while (ok && done < total) announce();
-    }
-  }
   } else if (warp < kWarpOut + 4 * H) {
     if constexpr (NC >= 96) take_registers<Regs<PAIR>::kMany>();
     // ---- accumulators to sums, sums to y -------------------------------------
