@@ -729,7 +729,8 @@ sph_status sph_fp8_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type,
  *          2^31, d <= 2^20.  The squares of a row add up within fp32's range.
  *   weight, bias  [d] of param_type (bf16, fp32 or fp16), each or NULL (1 and 0).
  *   eps    >= 0 and finite.
- *   out    [rows, d], row stride ld_out; may be x itself.
+ *   out    [rows, d], row stride ld_out; may be x itself, of its type and row
+ *          stride.
  *   mean, rstd    fp32 [rows] (out), what sph_layer_norm_grad takes, or NULL.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 sph_status sph_layer_norm(sph_ctx* ctx, const void* x, sph_tab_type x_type,
@@ -749,7 +750,8 @@ sph_status sph_layer_norm(sph_ctx* ctx, const void* x, sph_tab_type x_type,
  *   d_out  [rows, d] bf16, fp32 or fp16, row stride ld_d_out;  x, weight as given
  *          to sph_layer_norm.
  *   mean, rstd  fp32 [rows], what sph_layer_norm left; mean NULL: not centred.
- *   d_x    [rows, d], row stride ld_d_x; may be d_out or x itself.
+ *   d_x    [rows, d], row stride ld_d_x; may be d_out or x itself, of its type and
+ *          row stride.
  *   d_weight, d_bias  [d] of grad_type (out), each or NULL.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA, OOM. */
 sph_status sph_layer_norm_grad(sph_ctx* ctx, const void* d_out,
@@ -802,8 +804,8 @@ typedef struct sph_shaping {
  *   logits [rows, n_keep] bf16, fp32 or fp16, row stride ld_logits; rows >= 1.
  *   keep_ids, n_keep, V  as for sph_partial_logits.
  *   shaping  NULL for none of it.
- *   out    [rows, n_keep], row stride ld_out; may be logits itself.  fp32 where
- *          tokens are asked for.
+ *   out    [rows, n_keep], row stride ld_out; may be logits itself, of its type
+ *          and row stride.  fp32 where tokens are asked for.
  *   tokens int32 [rows] (out) vocabulary ids, or NULL.
  * A mask_rows entry outside [-1, n_masks) leaves the row unmasked, and sph_sync
  * reports SPH_ERR_INVALID_ARG.  SPH_OPT_SAMPLER = 1 is not supported here.

@@ -1627,6 +1627,12 @@ sph_status check_param(sph_ctx* ctx, const char* name, const void* p, int type) 
   if ((uintptr_t)p % tab_size(type)) return fail(ctx, SPH_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
   return SPH_OK;
 }
+// A result may take its input's place where each element does.
+sph_status check_place(sph_ctx* ctx, const char* name, const void* out, int out_type, int64_t ld_out,
+                       const char* from, const void* in, int in_type, int64_t ld_in, int64_t rows) {
+  if (out != in || (out_type == in_type && (ld_out == ld_in || rows < 2))) return SPH_OK;
+  return fail(ctx, SPH_ERR_INVALID_ARG, "%s in place of %s needs its type and row stride", name, from);
+}
 sph_status check_norm_rows(sph_ctx* ctx, int64_t rows, int64_t d) {
   if (rows < 0 || rows > INT32_MAX) return fail(ctx, SPH_ERR_INVALID_ARG, "rows=%lld out of [0, 2^31)", (long long)rows);
   return check_d(ctx, d);
@@ -1648,6 +1654,7 @@ sph_status sph_layer_norm(sph_ctx* ctx, const void* x, sph_tab_type x_type, int6
   if (rows == 0) return SPH_OK;
   st = check_rows(ctx, "x", x, x_type, d, ld_x);
   if (!st) st = check_rows(ctx, "out", out, out_type, d, ld_out);
+  if (!st) st = check_place(ctx, "out", out, out_type, ld_out, "x", x, x_type, ld_x, rows);
   if (st) return st;
   DeviceGuard g(ctx->device);
   if (!g.ok) return fail(ctx, SPH_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
@@ -1677,6 +1684,8 @@ sph_status sph_layer_norm_grad(sph_ctx* ctx, const void* d_out, sph_tab_type d_o
     st = check_rows(ctx, "d_out", d_out, d_out_type, d, ld_d_out);
     if (!st) st = check_rows(ctx, "x", x, x_type, d, ld_x);
     if (!st) st = check_rows(ctx, "d_x", d_x, d_x_type, d, ld_d_x);
+    if (!st) st = check_place(ctx, "d_x", d_x, d_x_type, ld_d_x, "d_out", d_out, d_out_type, ld_d_out, rows);
+    if (!st) st = check_place(ctx, "d_x", d_x, d_x_type, ld_d_x, "x", x, x_type, ld_x, rows);
     if (st) return st;
     if (!rstd) return fail(ctx, SPH_ERR_INVALID_ARG, "rstd must be non-NULL");
   }
@@ -1710,6 +1719,8 @@ sph_status sph_shape_logits(sph_ctx* ctx, const void* logits, sph_tab_type logit
   if (st) return st;
   st = check_rows(ctx, "logits", logits, logits_type, n_keep, ld_logits);
   if (!st) st = check_rows(ctx, "out", out, out_type, n_keep, ld_out);
+  if (!st)
+    st = check_place(ctx, "out", out, out_type, ld_out, "logits", logits, logits_type, ld_logits, rows);
   if (st) return st;
   if (n_keep > sph::sample_max_n()) return fail(ctx, SPH_ERR_UNSUPPORTED, "n_keep above %d", sph::sample_max_n());
   if (sph::shape_blocks(rows, (int)n_keep, ctx->sm_count) > INT32_MAX)

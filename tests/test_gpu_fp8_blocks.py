@@ -128,9 +128,12 @@ def test_borders_in_16_bits(sph, ctx, dtype):
         assert np.array_equal(bytes_of(w), codes)
 
 
-@pytest.mark.parametrize("dtype,bits", [(torch.bfloat16, 8), (torch.float16, 11)])
+@pytest.mark.parametrize("dtype,bits,power", [
+    (torch.bfloat16, 8, 0), (torch.bfloat16, 8, -127), (torch.bfloat16, 8, -118), (torch.bfloat16, 8, -69),
+    (torch.bfloat16, 8, 120), (torch.float16, 11, -6), (torch.float16, 11, -20), (torch.float16, 11, 4)])
 @pytest.mark.parametrize("block", [1, 128])
-def test_every_pair_of_mantissas(sph, ctx, dtype, bits, block):
+def test_every_pair_of_mantissas(sph, ctx, dtype, bits, power, block):
+    # (scales at and next to the least one, and from subnormal magnitudes, too)
     # quotients half way between two codes but for what rounding the scale took, and those that
     # are exact: every significand of x under every (fp16: every 17th) significand of amax
     half = 1 << bits - 1
@@ -149,7 +152,7 @@ def test_every_pair_of_mantissas(sph, ctx, dtype, bits, block):
         rows[:, ::2] *= -1
         rows[:, -1] = amax
         rows = rows.reshape(-1, 128)
-    rows = (rows * (2.0 ** -6 if bits == 11 else 1.0)).to(dtype).to(DEV)
+    rows = (rows * 2.0 ** power).to(dtype).to(DEV)
     w = ctx.fp8_quantize(rows, block)
     ctx.sync()
     codes, scales = ora.encode8(f64(rows), block)

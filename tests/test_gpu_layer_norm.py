@@ -190,6 +190,54 @@ def test_gradients_of_rows_of_any_length(ctx, R, d, dtype):
     assert all(torch.equal(a.view(torch.uint8), c.view(torch.uint8)) for a, c in zip(got, again))
 
 
+@pytest.mark.parametrize("R,d", [(5000, 40), (5000, 256), (2600, 512), (2000, 1000), (900, 1536),
+                                 (950, 4096), (701, 4104), (330, 5120), (320, 8192), (310, 12000)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("which", ["both", "none"])
+def test_many_rows_and_parameters_of_their_type(ctx, R, d, dtype, which):
+    # more rows than blocks, so that each takes several; all of one type
+    def equal(one, two):
+        return all((a is None and c is None) or torch.equal(a.view(torch.uint8), c.view(torch.uint8))
+                   for a, c in zip(one, two))
+
+    def grads(dy, x, d_x=None):
+        sums = dict(d_bias=torch.empty(d, device=DEV))
+        if w is not None:
+            sums["d_weight"] = torch.empty(d, device=DEV)
+        return ctx.layer_norm_grad(dy, x, w, mean, rstd, d_x=d_x, **sums)
+
+    x, dy = rows_of(R, d, dtype, R + d), rows_of(R, d, dtype, R + d + 1, offset=0.1)
+    w, b = params(d, dtype, d) if which == "both" else (None, None)
+    y, mean, rstd = ctx.layer_norm(x, w, b, stats=True)
+    got, again = grads(dy, x), grads(dy, x)
+    ctx.sync()
+    check_y(y, x, w, b, True, 1e-5, dtype)
+    check_grads(got, dy, x, w, mean, rstd, (dtype, torch.float32))
+    assert equal(got, again)
+    # in place of the rows, and of their gradient
+    at_x, at_dy = x.clone(), dy.clone()
+    assert equal(got, grads(dy, at_x, at_x)) and equal(got, grads(at_dy, x, at_dy))
+    ctx.layer_norm(x, w, b, out=x)
+    ctx.sync()
+    assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def test_in_place_needs_the_same_form(sph, ctx):
+    x = rows_of(4, 64, torch.float32, 1)
+    _, mean, rstd = ctx.layer_norm(x, stats=True)
+    was, half = x.clone(), x.view(torch.bfloat16)[:, :64]
+    wide = x.view(-1)[:3 * 64].view(3, 64)
+    for call in (lambda: ctx.layer_norm(x, out=half), lambda: ctx.layer_norm(wide[:2], out=x[::2]),
+                 lambda: ctx.layer_norm_grad(x, was, None, mean, rstd, d_x=half),
+                 lambda: ctx.layer_norm_grad(was, x, None, mean, rstd, d_x=half)):
+        with pytest.raises(sph.SphError):
+            call()
+    ctx.sync()
+    assert torch.equal(x, was)
+    ctx.layer_norm(x[:1], out=x[::4])                # one row: any stride
+    ctx.sync()
+
+
 @pytest.mark.parametrize("d", [33, 600, 4096, 9000])
 @pytest.mark.parametrize("centre", [True, False])
 @pytest.mark.parametrize("xt,yt,ot,gt", [(0, 1, 2, 0), (1, 0, 1, 1), (2, 1, 0, 2), (1, 2, 1, 0)])

@@ -143,6 +143,17 @@ def test_each_alone_and_none(ctx, what, n):
             assert same(y.cpu().numpy(), ora.shape(z, n, **b, dtype=np.float32))
 
 
+def test_in_place_needs_the_same_form(sph, ctx):
+    z = torch.randn(4, 64, device=DEV)
+    was = z.clone()
+    for call in (lambda: ctx.shape_logits(z, 64, out=z.view(torch.bfloat16)[:, :64]),
+                 lambda: ctx.shape_logits(z[:2], 64, out=z[::2])):
+        with pytest.raises(sph.SphError):
+            call()
+    ctx.sync()
+    assert torch.equal(z, was)
+
+
 def test_masks_by_index_and_in_place(ctx):
     z, a = make(9, 3000, 3000, 7, mask_rows=True)
     zd = dev(z, torch.float32)
