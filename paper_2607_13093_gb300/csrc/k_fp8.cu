@@ -244,7 +244,8 @@ __global__ void __launch_bounds__(kLookThreads) fp8_lookup_kernel(const Fp8Looku
   if (!there && id != a.padding && span == 0 && lane == 0) atomicOr(a.status, ERR_BAD_INDEX);
   OT* out = static_cast<OT*>(a.out) + t * a.ld_out;
   const uint8_t* row = there ? a.codes + id * a.ld_codes : nullptr;
-  const float* scales = there ? a.scales + id / a.block_rows * a.ld_scales : nullptr;
+  const float* scales =
+      there ? a.scales + (a.block_rows == 1 ? id : id / kFp8Block) * a.ld_scales : nullptr;
   if constexpr (!ON16) {
     const int col = span * 32 * kCols + lane;
     if (col + 31 * kCols >= a.d || !there) {
@@ -266,12 +267,9 @@ __global__ void __launch_bounds__(kLookThreads) fp8_lookup_kernel(const Fp8Looku
   const int col = span * 32 * kCols + lane * kCols;
   if (col >= a.d) return;
   float v[2][8];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[h][j] = 0.f;
+  uint32_t w[4] = {0, 0, 0, 0};
+  float s = 0.f;
   if (there) {
-    uint32_t w[4] = {0, 0, 0, 0};
     if (col + kCols <= a.d) {
       const uint4 c = *reinterpret_cast<const uint4*>(row + col);
       w[0] = c.x; w[1] = c.y; w[2] = c.z; w[3] = c.w;
@@ -280,15 +278,18 @@ __global__ void __launch_bounds__(kLookThreads) fp8_lookup_kernel(const Fp8Looku
       for (int j = 0; j < kCols; ++j)
         if (col + j < a.d) w[j / 4] |= (uint32_t)row[col + j] << 8 * (j % 4);
     }
-    const float s = scales[col / kFp8Block];
+    s = scales[col / kFp8Block];
+  }
+  // (a row that is not there: zeros times 0 times 1)
+  const F2 s2 = f2(s), by = f2(there ? a.scale : 1.f);
 #pragma unroll
-    for (int j = 0; j < kCols; j += 2) {
-      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(
-          (__nv_fp8x2_storage_t)(w[j / 4] >> 8 * (j % 4) & 0xFFFFu), __NV_E4M3);
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-      v[j / 8][j % 8] = f.x * s * a.scale;
-      v[j / 8][j % 8 + 1] = f.y * s * a.scale;
-    }
+  for (int j = 0; j < kCols; j += 2) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(
+        (__nv_fp8x2_storage_t)(w[j / 4] >> 8 * (j % 4) & 0xFFFFu), __NV_E4M3);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    const float2 r = both(mul2(mul2(f2(f.x, f.y), s2), by));
+    v[j / 8][j % 8] = r.x;
+    v[j / 8][j % 8 + 1] = r.y;
   }
   if (col + kCols <= a.d && on32(out + col)) {
     if constexpr (sizeof(OT) == 4) {
