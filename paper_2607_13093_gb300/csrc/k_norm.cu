@@ -11,8 +11,8 @@
 // is small and its threads hold several pieces, so that many rows are on their way to an SM at
 // once and few threads wait for each other: 16384 x 5120 bf16 62 us (5.4 TB/s), fp32 97 us (6.9
 // TB/s).  320 threads a row took 98 us, a ring of rows in shared memory that two groups of these
-// took in turn 171, and a branch on each type in every piece 74 (a quarter of the stalls were
-// waits for code).  Rows at any address: 16384 x 5119 bf16 101 us.  Of few rows a block has as many
+// took in turn 171, and pieces with the code for rows at any address beside the aligned one's 74
+// (a quarter of the stalls were waits for code).  Rows at any address: 16384 x 5119 bf16 101 us.  Of few rows a block has as many
 // threads as there are pieces: 500 x 4096 bf16 4.8 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -191,6 +191,8 @@ cudaError_t launch_norm_v(const Norm& a, int sm_count, cudaStream_t st) {
 }
 template <class T>
 cudaError_t launch_norm_t(const Norm& a, int mode, int sm_count, cudaStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (mode == 3) return launch_norm_v<T, 3>(a, sm_count, st);
   return mode == 2   ? launch_norm_v<T, 2>(a, sm_count, st)
          : mode == 1 ? launch_norm_v<T, 1>(a, sm_count, st)
                      : launch_norm_v<T, 0>(a, sm_count, st);
@@ -202,8 +204,12 @@ cudaError_t launch_norm(const Norm& a, int x_type, int sm_count, cudaStream_t st
   const bool wide = a.d % 8 == 0 && wide_rows(a.x, a.ld_x, x_type) &&
                     wide_rows(a.out, a.ld_out, a.out_type) && wide_rows(a.weight, 0, a.param_type) &&
                     wide_rows(a.bias, 0, a.param_type);
-  const bool same = a.out_type == x_type && (a.param_type == x_type || (!a.weight && !a.bias));
-  const int mode = !wide ? 0 : same ? 2 : 1;
+  const bool none = !a.weight && !a.bias, same = none || a.param_type == x_type;
+  const int mode = !wide                                    ? 0
+                   : a.out_type != x_type                   ? 1
+                   : same                                   ? 2
+                   : a.param_type == TAB_FP32               ? 3
+                                                            : 1;
   if (x_type == TAB_FP32) return launch_norm_t<float>(a, mode, sm_count, st);
   if (x_type == TAB_BF16) return launch_norm_t<__nv_bfloat16>(a, mode, sm_count, st);
   return launch_norm_t<__half>(a, mode, sm_count, st);

@@ -89,7 +89,6 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
   // n and g of a row stay in registers over the exchange; else both are made twice (where they
   // do not fit without spills: fp32 16384 x 4096 141 us so, 151 held)
   constexpr bool HOLD = RING && U <= 2;
-  constexpr bool KEEP = MODE == 2 && sizeof(TX) == 2;      // the weight stays in registers
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int threads = WARP ? 32 : (int)blockDim.x;
@@ -103,29 +102,31 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
 #pragma unroll
     for (int k = 0; k < 4; ++k) sw[i][k] = sb[i][k] = f2(0.f);
 
-  Eight<TX, M> w[KEEP ? U : 1];
-  if constexpr (KEEP) {
+  // the weight in fp32, in shared memory: each thread its own columns
+  float4* const w_places = reinterpret_cast<float4*>(smem) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int col = piece_col<MODE>(i, t, threads);
-      w[i].ones();
-      if (a.weight && col < a.d) w[i].load(static_cast<const TX*>(a.weight), col, a.d);
+  for (int i = 0; i < U; ++i) {
+    const int col = piece_col<MODE>(i, t, threads);
+    if (col >= a.d) break;
+    F2 p[4] = {f2(1.f), f2(1.f), f2(1.f), f2(1.f)};
+    if (a.weight) load_param<TX, M>(a.weight, a.weight_type, col, a.d, p);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float2 lo = both(p[2 * k]), hi = both(p[2 * k + 1]);
+      w_places[(2 * i + k) * (int)blockDim.x] = make_float4(lo.x, lo.y, hi.x, hi.y);
     }
   }
-  auto weight = [&](int i, int col, F2 (&p)[4]) {
-    if constexpr (KEEP) {
+  auto weight = [&](int i, F2 (&p)[4]) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) p[k] = w[i].two(k);
-    } else if (a.weight) {
-      load_param<TX, MODE>(a.weight, a.weight_type, col, a.d, p);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) p[k] = f2(1.f);
+    for (int k = 0; k < 2; ++k) {
+      const float4 q = w_places[(2 * i + k) * (int)blockDim.x];
+      p[2 * k] = f2(q.x, q.y);
+      p[2 * k + 1] = f2(q.z, q.w);
     }
   };
 
   constexpr int kPlaces = U * 16;             // of a thread, for a row of x or dy
-  unsigned char* const way = smem + (WARP ? (threadIdx.x >> 5) * kDepth * 2 * kPlaces * 32 : 0);
+  unsigned char* const way = smem + U * 32 * blockDim.x + (WARP ? (threadIdx.x >> 5) * kDepth * 2 * kPlaces * 32 : 0);
   auto ask = [&](int64_t row, int slot) {
     if constexpr (RING) {
       if (row < a.rows) {
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
       const int col = piece_col<MODE>(i, t, threads);
       if (col >= a.d) break;
       F2 p[4];
-      weight(i, col, p);
+      weight(i, p);
       // (behind the row's end dy reads as zero, and n is -mean rstd: finite if the row's is)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
       const int at = HOLD ? i : 0;
       if constexpr (!HOLD) {
         F2 p[4];
-        weight(i, col, p);
+        weight(i, p);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           n[0][k] = n_of(i, k);
@@ -428,7 +429,8 @@ cudaError_t launch_grad_v(const NormGrad& a, const GradPlan& p, cudaStream_t st)
   auto go = [&](auto kernel) {
     const int on_way = MODE && packed ? kDepth * p.u * 32 * p.threads : 0;
     const int sums = p.warps ? p.u * 64 * 128 : 0;
-    const int smem = on_way > sums ? on_way : sums;
+    const int weights = p.u * 32 * p.threads;
+    const int smem = weights + on_way > sums ? weights + on_way : sums;
     if (smem > 40 * 1024) {         // (48 KB hold the static part too)
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
       if (e != cudaSuccess) return e;
