@@ -9,11 +9,11 @@
 // Bound by memory: x is read once and y written.  A row belongs to a warp (up to 1024 columns)
 // or a block, whose threads hold eight columns a piece as they were read.  Of many rows a block
 // is small and its threads hold several pieces, so that many rows are on their way to an SM at
-// once and few threads wait for each other: 16384 x 5120 bf16 62 us (5.4 TB/s), fp32 97 us (6.9
+// once and few threads wait for each other: 16384 x 5120 bf16 56 us (6.0 TB/s), fp32 97 us (6.9
 // TB/s).  320 threads a row took 98 us, a ring of rows in shared memory that two groups of these
 // took in turn 171, and pieces with the code for rows at any address beside the aligned one's 74
-// (a quarter of the stalls were waits for code).  Rows at any address: 16384 x 5119 bf16 101 us.  Of few rows a block has as many
-// threads as there are pieces: 500 x 4096 bf16 4.8 us.
+// (a quarter of the stalls were waits for code).  Rows at any address: 16384 x 5119 bf16 101 us.
+// Of few rows a block has as many threads as there are pieces: 500 x 4096 bf16 4.0 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

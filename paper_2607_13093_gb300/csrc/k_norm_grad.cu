@@ -11,9 +11,11 @@
 // inputs give equal bits.  With the sums in registers few warps find room, so the next rows
 // are on their way while one is worked on: 16-bit rows three ahead in shared memory, which each
 // thread fills and reads by itself (no barrier), fp32 rows one ahead in registers (in shared
-// memory 201 us, the two halves of a thread's 32 bytes being two requests of every sector).
-// 32768 x 4096 bf16 174 us (4.6 TB/s), fp32 16384 x 4096 142 us (5.7 TB/s).  Rows at any address
-// are read 32 columns an access, two or four bytes a lane: 32768 x 4095 bf16 327 us.
+// memory 201 us, the two halves of a thread's 32 bytes being two requests of every sector).  The
+// weight lies in shared memory in fp32, each thread's own columns (read and converted for each
+// row 175 us, kept in registers 194).
+// 32768 x 4096 bf16 143 us (5.6 TB/s), fp32 16384 x 4096 136 us (5.9 TB/s).  Rows at any address
+// are read 32 columns an access, two or four bytes a lane: 32768 x 4095 bf16 282 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -83,12 +85,11 @@ template <class TX, class TY, int U, int MODE, bool WARP, int THREADS, int BLOCK
 __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGrad a) {
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float red[2][32];
-  constexpr int M = MODE ? 1 : 0;
   // 16-bit rows through shared memory; others a row ahead in registers
   constexpr bool RING = MODE != 0 && sizeof(TX) + sizeof(TY) == 4, AHEAD = MODE != 0 && !RING;
-  // n and g of a row stay in registers over the exchange; else both are made twice (where they
-  // do not fit without spills: fp32 16384 x 4096 141 us so, 151 held)
-  constexpr bool HOLD = RING && U <= 2;
+  // n and g of a row stay in registers over the exchange; else, where they do not fit without
+  // spills, both are made twice (fp32 16384 x 4096 141 us so, 151 held)
+  constexpr bool HOLD = RING;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int threads = WARP ? 32 : (int)blockDim.x;
@@ -109,7 +110,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
     const int col = piece_col<MODE>(i, t, threads);
     if (col >= a.d) break;
     F2 p[4] = {f2(1.f), f2(1.f), f2(1.f), f2(1.f)};
-    if (a.weight) load_param<TX, M>(a.weight, a.weight_type, col, a.d, p);
+    if (a.weight) load_param<TX, MODE>(a.weight, a.weight_type, col, a.d, p);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const float2 lo = both(p[2 * k]), hi = both(p[2 * k + 1]);
@@ -139,8 +140,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
     }
   };
   struct Row {
-    Eight<TX, M> x[U];
-    Eight<TY, M> y[U];
+    Eight<TX, MODE> x[U];
+    Eight<TY, MODE> y[U];
   };
   auto read = [&](int64_t row, Row& to) {
 #pragma unroll
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
           v[k] = add2(v[k], f2(q.x, q.y));
         }
       }
-      store_eight<float, M>(a.partial, ((int64_t)blockIdx.x * 2 + warp) * a.ld_partial, col, a.d, v);
+      store_eight<float, MODE>(a.partial, ((int64_t)blockIdx.x * 2 + warp) * a.ld_partial, col, a.d, v);
     }
   } else {
     float* pw = a.partial + (int64_t)owner * 2 * a.ld_partial;
@@ -270,8 +271,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
     for (int i = 0; i < U; ++i) {
       const int col = piece_col<MODE>(i, t, threads);
       if (col >= a.d) break;
-      store_eight<float, M>(pw, 0, col, a.d, sw[i]);
-      store_eight<float, M>(pw, a.ld_partial, col, a.d, sb[i]);
+      store_eight<float, MODE>(pw, 0, col, a.d, sw[i]);
+      store_eight<float, MODE>(pw, a.ld_partial, col, a.d, sb[i]);
     }
   }
 }
@@ -389,10 +390,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(const NormGr
   *out = from_f32<T>(a.accumulate ? to_f32(*out) + v : v);
 }
 
-// How a call's rows are divided.  packed: x and dy have 16 bits, and a warp holds rows of up to
-// 1024 columns; ring: they come through shared memory.  Blocks of 256 threads: two an SM, whose
-// threads hold n and g (32768 x 4096 bf16 174 us; three that make both twice 196, threads of four
-// pieces 220); rows at any address three (325 us, two 383).
+// How a call's rows are divided.  packed: x and dy have 16 bits; ring: they come through shared
+// memory.  Blocks of 256 threads: two an SM, whose threads hold n and g (three that make both
+// twice: 32768 x 4096 bf16 196 us where two took 174, threads of four pieces 220); rows at any
+// address three (325 us, two 383).  Rows of 512 to 1024 columns by blocks too (60000 x 1000 75 us,
+// by warps of four pieces 92).
 struct GradPlan {
   bool warps, is_long;
   int u, threads, parts;
@@ -401,11 +403,11 @@ GradPlan grad_plan(int64_t rows, int d, bool packed, bool ring, int sm_count) {
   GradPlan p{};
   const int64_t sms = sm_count;
   int64_t most;
-  if (d <= 32 * (packed ? 32 : 16)) {
+  if (d <= 32 * 16) {
     p.warps = true;
-    p.u = d <= 32 * 8 ? 1 : d <= 32 * 16 ? 2 : 4;
+    p.u = d <= 32 * 8 ? 1 : 2;
     p.threads = 128;
-    most = sms * (!packed ? 4 : p.u == 1 ? 8 : p.u == 2 ? 4 : 3);
+    most = sms * (packed && p.u == 1 ? 6 : 4);
     rows = (rows + 3) / 4;
   } else if (d <= kMaxThreads * 16) {
     // (few rows: as many threads as a row has)
@@ -438,12 +440,11 @@ cudaError_t launch_grad_v(const NormGrad& a, const GradPlan& p, cudaStream_t st)
     return launch_pdl(kernel, dim3((unsigned)p.parts), dim3((unsigned)p.threads), smem, st, a);
   };
   if constexpr (packed) {
-    if (p.u == 4) return go(norm_grad_kernel<TX, TY, 4, MODE, true, 128, 3>);
     if (p.u == 2 && !p.warps && p.threads <= 256)
       return go(norm_grad_kernel<TX, TY, 2, MODE, false, 256, MODE ? 2 : 3>);
   }
   if (p.warps)
-    return p.u == 1 ? go(norm_grad_kernel<TX, TY, 1, MODE, true, 128, packed ? 8 : 4>)
+    return p.u == 1 ? go(norm_grad_kernel<TX, TY, 1, MODE, true, 128, packed ? 6 : 4>)
                     : go(norm_grad_kernel<TX, TY, 2, MODE, true, 128, 4>);
   return p.u == 1 ? go(norm_grad_kernel<TX, TY, 1, MODE, false, kMaxThreads, 1>)
                   : go(norm_grad_kernel<TX, TY, 2, MODE, false, kMaxThreads, 1>);
@@ -451,8 +452,6 @@ cudaError_t launch_grad_v(const NormGrad& a, const GradPlan& p, cudaStream_t st)
 template <class TX, class TY>
 cudaError_t launch_grad_y(const NormGrad& a, const GradPlan& p, int mode, cudaStream_t st) {
   if (!p.is_long) {
-    if constexpr (std::is_same<TX, TY>::value)
-      if (mode == 2) return launch_grad_v<TX, TY, 2>(a, p, st);
     return mode ? launch_grad_v<TX, TY, 1>(a, p, st) : launch_grad_v<TX, TY, 0>(a, p, st);
   }
   if (a.partial) {
@@ -492,8 +491,7 @@ cudaError_t launch_norm_grad(NormGrad a, int x_type, int dy_type, int grad_type,
   const bool wide = a.d % 8 == 0 && wide_rows(a.x, a.ld_x, x_type) &&
                     wide_rows(a.dy, a.ld_dy, dy_type) && wide_rows(a.dx, a.ld_dx, a.dx_type) &&
                     wide_rows(a.weight, 0, a.weight_type);
-  const bool same = dy_type == x_type && a.dx_type == x_type && (!a.weight || a.weight_type == x_type);
-  const int mode = !wide ? 0 : same ? 2 : 1;
+  const int mode = wide ? 1 : 0;
   const bool packed = x_type != TAB_FP32 && dy_type != TAB_FP32;
   const GradPlan p = grad_plan(a.rows, a.d, packed, packed && mode, sm_count);
   a.parts = p.parts;

@@ -15,9 +15,10 @@ namespace sph {
 //      wherever the row starts;
 //   1  d is a multiple of 8, and all rows and parameters are on 16 bytes (fp32: 32): the eight
 //      are neighbours, read and written in one access;
-//   2  the same, and parameters and results have the type of x (and dy): no branch on a type
-//      (16384 x 5120 bf16 59.3 us, 62.3 with one; 10000 x 8192 57.4 and 69.8);
-//   3  the same with fp32 parameters.
+//   2  (the norm alone) the same, and parameters and results have the type of x: no branch on a
+//      type;
+//   3  the same with fp32 parameters (16384 x 5120 bf16 56 us, with a branch 62; 10000 x 8192 58
+//      and 70).
 template <int MODE>
 __device__ __forceinline__ int piece_col(int i, int t, int threads) {
   return MODE ? (i * threads + t) * 8 : (i * threads + (t & ~31)) * 8 + (t & 31);
