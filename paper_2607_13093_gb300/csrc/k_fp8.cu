@@ -260,7 +260,8 @@ __global__ void __launch_bounds__(kLookThreads) fp8_lookup_kernel(const Fp8Looku
     for (int j = 0; j < kCols; j += kFp8Block / 32) {
       const float s = scales[(col + 32 * j) / kFp8Block];
 #pragma unroll
-      for (int k = j; k < j + kFp8Block / 32; ++k) out[col + 32 * k] = from_f32<OT>(value_of(w[k]) * s * a.scale);
+      for (int k = j; k < j + kFp8Block / 32; ++k)
+        out[col + 32 * k] = from_f32<OT>(value_of(w[k]) * s * a.scale);
     }
     return;
   }

@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
   };
 
   constexpr int kPlaces = U * 16;             // of a thread, for a row of x or dy
-  unsigned char* const way = smem + U * 32 * blockDim.x + (WARP ? (threadIdx.x >> 5) * kDepth * 2 * kPlaces * 32 : 0);
+  unsigned char* const way = smem + U * 32 * blockDim.x +
+                             (WARP ? (threadIdx.x >> 5) * kDepth * 2 * kPlaces * 32 : 0);
   auto ask = [&](int64_t row, int slot) {
     if constexpr (RING) {
       if (row < a.rows) {
