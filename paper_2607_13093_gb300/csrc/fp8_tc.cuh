@@ -93,6 +93,13 @@ __device__ __forceinline__ uint64_t fma2_here(uint64_t a, uint64_t b, uint64_t c
   asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
+// A scale, at most the largest finite value: what stands for a product past the range stays
+// finite for a sum of zero.  A NaN's block has codes of zero, and its NaN must not get lost here.
+__device__ __forceinline__ float bounded(float x) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(3.402823466e38f));
+  return r;
+}
 // Four rows by one copy, to a pair (bar: a shared::cluster address).
 __device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int x, int4 rows,
                                             uint32_t bar) {

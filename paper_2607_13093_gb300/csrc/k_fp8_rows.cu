@@ -293,8 +293,7 @@ fp8_rows_as_m_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
           auto add = [&](int q, uint32_t (&of)[kGroup]) {
             const float w0 = w[GATHER ? q : 0][0], w1 = w[GATHER ? q : 0][kEnds - 1];
             if constexpr (FAR) {
-              // where W's scale is far from 1 a factor of 2^64 goes from it to X's (whose
-              // product past the range has to stay finite for a sum of zero)
+              // where W's scale is far from 1 a factor of 2^64 goes from it to X's
 #pragma unroll
               for (int i = 0; i < kGroup; ++i) {
                 float s = GATHER && i >= split[q] ? w1 : w0, lift = 1.f;
@@ -305,7 +304,7 @@ fp8_rows_as_m_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_con
                 if (fabsf(s) > kFar) { lift = 0x1p64f; s *= 0x1p-64f; }
                 else if (fabsf(s) < kNear && s != 0.f) { lift = 0x1p-64f; s *= 0x1p64f; }
                 const float part = __fmul_rn(__uint_as_float(of[i]), s);
-                sum[q * kGroup + i] = __fmaf_rn(part, fminf(x * lift, 3.402823466e38f), sum[q * kGroup + i]);
+                sum[q * kGroup + i] = __fmaf_rn(part, bounded(x * lift), sum[q * kGroup + i]);
               }
             } else {
               const float f0 = x * w0, f1 = x * w1;

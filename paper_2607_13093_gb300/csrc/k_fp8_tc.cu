@@ -377,9 +377,7 @@ fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
           } else {
 #pragma unroll
             for (int i = 0; i < G / 2; ++i) {
-              // (a product past the range has to stay finite for a sum of zero)
-              const float s0 = fminf(sx[q * G + 2 * i] * lift, 3.402823466e38f);
-              const float s1 = fminf(sx[q * G + 2 * i + 1] * lift, 3.402823466e38f);
+              const float s0 = bounded(sx[q * G + 2 * i] * lift), s1 = bounded(sx[q * G + 2 * i + 1] * lift);
               uint64_t& at = sum[(q * G + 2 * i) / 2];
               at = fma2_here(mul2(pack2(of[2 * i], of[2 * i + 1]), sw2), pack2(s0, s1), at);
             }

@@ -341,6 +341,32 @@ def test_nan_blocks_stay_in_their_rows_and_ids(sph, ctx):
     assert torch.equal(y.isnan(), bad)
 
 
+@pytest.mark.parametrize("pair", [0, 1, 2])
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("block,rows", [(1, 5), (1, 40), (1, 100), (1, 260), (128, 5), (128, 40),
+                                        (128, 130), (128, 260)])
+def test_bad_hidden_states_beside_zero_rows(sph, pair, kept, block, rows):
+    # a NaN or an infinity of a hidden state reaches each of its logits, and no other's, whatever
+    # the table's scales and the number of rows: those of zeros have 2^-126
+    V, d = 700, 300
+    table = make_x(V, d, torch.float32, 7)
+    table[7], table[256:384] = 0, 0
+    h = make_x(rows, d, torch.float32, rows)
+    h[1, 70], h[3, 299], h[rows - 1, 0], h[2] = float("nan"), float("inf"), float("-inf"), 0
+    bad = torch.tensor(sorted({1, 3, rows - 1}), device=DEV)
+    good = torch.tensor([r for r in range(rows) if r not in (1, 3, rows - 1)], device=DEV)
+    ids = np.concatenate([np.arange(100), np.arange(101, 300, 2), np.arange(350, 390), [600]])
+    ids = torch.tensor(ids.astype(np.int32), device=DEV) if kept else None
+    c = sph.Context(0)
+    c.set_option(sph.SPH_OPT_TC_PAIR, pair)
+    w = c.fp8_quantize(table, block)
+    y = c.fp8_logits(h, w, keep_ids=ids)
+    c.sync()
+    assert y[bad].isnan().all()
+    check(y[good], h[good], ora.decode8(bytes_of(w), w.scales.cpu().numpy(), block), ids)
+    c.close()
+
+
 def test_a_wait_that_gives_up(sph, ctx):
     c = sph.Context(0)
     for pair, block, rows in ((2, 1, 9), (1, 1, 9), (0, 128, 90)):
