@@ -1,5 +1,6 @@
 // C-ABI layer of libsph: context, scratch arena, argument validation and
 // dispatch of the split-head kernels.  Declared in include/sph.h.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -105,6 +106,9 @@ struct DeviceGuard {
       cudaSetDevice(prev);
   }
 };
+
+// Columns that the operators on a vocabulary table and on rows take at most.
+constexpr int64_t kTabMaxD = 1 << 20;
 
 // Grow the scratch arena to `bytes` (outside stream capture only).
 sph_status ensure_scratch(sph_ctx* ctx, size_t bytes) {
@@ -758,17 +762,18 @@ sph_status sph_reserve(sph_ctx* ctx, int64_t max_rows, int64_t max_n_keep,
   if (f > need) need = f;
   const size_t v = verify_reserve_bytes(max_rows, max_n_keep);
   if (v > need) need = v;
-  // the operators on a vocabulary table
-  const size_t m = sph::mx4_gemm_reserve_bytes(max_rows, max_n_keep, max_d, ctx->sm_count);
+  // the operators on a vocabulary table and on rows, which take no more ids and columns
+  const int64_t ids = std::min<int64_t>(max_n_keep, sph::sample_max_n());
+  const int64_t cols = std::min(max_d, kTabMaxD);
+  const size_t m = sph::mx4_gemm_reserve_bytes(max_rows, ids, cols, ctx->sm_count);
   if (m > need) need = m;
-  const size_t t = sph::grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
+  const size_t t = sph::grad_reserve_bytes(max_rows, cols, ctx->sm_count);
   if (t > need) need = t;
-  const size_t q = sph::fp8_gemm_reserve_bytes(max_rows, max_n_keep, max_d);
+  const size_t q = sph::fp8_gemm_reserve_bytes(max_rows, ids, cols);
   if (q > need) need = q;
-  // the operators on rows
-  const size_t n = sph::norm_grad_reserve_bytes(max_rows, max_d, ctx->sm_count);
+  const size_t n = sph::norm_grad_reserve_bytes(max_rows, cols, ctx->sm_count);
   if (n > need) need = n;
-  const size_t s = sph::shape_reserve_bytes(max_rows, max_n_keep);
+  const size_t s = sph::shape_reserve_bytes(max_rows, ids);
   if (s > need) need = s;
   for (int act = 0; act < 2; ++act) {      // a one-chunk split step
     const size_t a = split_scratch_bytes(ctx, max_rows, max_n_keep, max_n_keep, max_d, max_d,
@@ -1294,7 +1299,7 @@ sph_status sph_split_step(sph_ctx* ctx, const float* h, int64_t rows, int64_t ld
 // ---- operators on a vocabulary table ----------------------------------------
 namespace {
 
-constexpr int64_t kTabMaxD = 1 << 20, kTabMaxRows = 1 << 20;
+constexpr int64_t kTabMaxRows = 1 << 20;
 
 int tab_size(int t) { return t == SPH_TAB_FP32 ? 4 : 2; }
 bool tab_dense(int t) { return t == SPH_TAB_BF16 || t == SPH_TAB_FP32 || t == SPH_TAB_FP16; }

@@ -354,6 +354,23 @@ def test_far_rows(ctx):
     assert ((db.double() - total).abs() <= 4096 * U * mag).all()
 
 
+def test_reserve_for_more_columns_than_a_call_takes(sph, ctx):
+    x, dy = rows_of(1, 300, torch.float32, 1), rows_of(1, 300, torch.float32, 2)
+    w, _ = params(300, torch.float32, 3)
+    _, mean, rstd = ctx.layer_norm(x, w, stats=True)
+    want = ctx.layer_norm_grad(dy, x, w, mean, rstd)
+    own = sph.Context(0)
+    own.reserve(1, 1, 1 << 31)
+    own.reserve(1, 1, (1 << 31) + 4096)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = own.layer_norm_grad(dy, x, w, mean, rstd)
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    own.close()
+
+
 def test_other_streams_and_graphs(sph, ctx):
     R, d = 333, 1500
     x, dy = rows_of(R, d, torch.bfloat16, 1), rows_of(R, d, torch.bfloat16, 2)
