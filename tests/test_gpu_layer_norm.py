@@ -354,6 +354,31 @@ def test_far_rows(ctx):
     assert ((db.double() - total).abs() <= 4096 * U * mag).all()
 
 
+@pytest.mark.parametrize("d", [2100, 2104])
+def test_the_weights_gradient_over_far_rows(ctx, d):
+    # 2^20 rows and offsets past 2^31 elements, rows off 16 bytes and on them: blocks add some
+    # 2^11 rows each (152 SMs, three or four blocks an SM), then come 2^9 blocks; in each term
+    # one rounding for the difference and one for the product
+    R = (1 << 20) + 5
+    g = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.empty(R, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    dy = torch.empty(R, d, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    _, mean, rstd = ctx.layer_norm(x, stats=True)
+    _, dw, db = ctx.layer_norm_grad(dy, x, torch.ones(d, device=DEV), mean, rstd)
+    ctx.sync()
+    want = torch.zeros(2, d, dtype=torch.float64, device=DEV)
+    mag = torch.zeros(2, d, dtype=torch.float64, device=DEV)
+    for a in range(0, R, 1 << 17):
+        at = slice(a, a + (1 << 17))
+        n = (x[at].double() - mean[at].double()[:, None]) * rstd[at].double()[:, None]
+        y = dy[at].double()
+        for k, terms in enumerate((y * n, y)):
+            want[k] += terms.sum(0)
+            mag[k] += terms.abs().sum(0)
+    for k, got in enumerate((dw, db)):
+        assert ((got.double() - want[k]).abs() <= 4096 * U * mag[k]).all()
+
+
 def test_reserve_for_more_columns_than_a_call_takes(sph, ctx):
     x, dy = rows_of(1, 300, torch.float32, 1), rows_of(1, 300, torch.float32, 2)
     w, _ = params(300, torch.float32, 3)
