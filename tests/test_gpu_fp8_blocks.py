@@ -386,6 +386,32 @@ def test_a_wait_that_gives_up(sph, ctx):
     c.close()
 
 
+@pytest.mark.parametrize("pair,rows", [(1, 230), (2, 130)])
+@pytest.mark.parametrize("kept", [False, True])
+def test_a_wait_that_gives_up_with_many_hidden_states(sph, pair, rows, kept):
+    # hidden states as the MMA's M, and the tiles of scales far from 1 after them
+    V, d = 900, 1000
+    table = make_x(V, d, torch.float32, 3)
+    table[256:384] = 0
+    h = make_x(rows, d, torch.float32, 1)
+    ids = torch.tensor([i for i in range(V) if i % 5 or i < 300], dtype=torch.int32, device=DEV) if kept else None
+    c = sph.Context(0)
+    w = c.fp8_quantize(table, 128)
+    c.sync()
+    c.set_option(sph.SPH_OPT_TC_PAIR, pair)
+    for _ in range(2):
+        c.set_option(sph.SPH_OPT_SPIN_LIMIT, 1)
+        c.fp8_logits(h, w, keep_ids=ids)
+        with pytest.raises(sph.SphError) as e:
+            c.sync()
+        assert e.value.status == 4
+        c.set_option(sph.SPH_OPT_SPIN_LIMIT, 1 << 34)
+        y = c.fp8_logits(h, w, keep_ids=ids)
+        c.sync()
+        check(y, h, ora.decode8(bytes_of(w), w.scales.cpu().numpy(), 128), ids)
+    c.close()
+
+
 def test_streams_graphs_and_reserve(sph, ctx):
     V, d, rows = 500, 300, 20
     w, table = held(ctx, V, d, 128, 4)
