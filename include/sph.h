@@ -702,7 +702,12 @@ sph_status sph_embed_fp8(sph_ctx* ctx, const int32_t* tokens, int64_t n_tokens,
  * where qx, sx are h quantised as sph_fp8_quantize does with block_rows 1, and qw,
  * sw the table's codes and scales.  A block's sum and the sum over blocks are
  * fp32: a logit is finite wherever the magnitudes of its products add up within
- * fp32's range, whatever the scales.
+ * fp32's range, whatever the scales; a block that stands for NaN makes every logit
+ * that it enters NaN.
+ * Scales of 128 rows and many hidden states: tiles with a scale outside
+ * [2^-50, 2^50] (a block of zeros has 2^-126), or with a group of 32 kept ids that
+ * meets three blocks of 128 rows or more, are computed twice, the second time more
+ * slowly.  Where many are like that SPH_OPT_TC_PAIR 2 is faster.
  *   h      [rows, W->d] bf16, fp32 or fp16, row stride ld_h elements.
  *   bias   fp32 [W->rows] or NULL.  keep_ids, n_keep as for
  *          sph_partial_logits, with V = W->rows.
@@ -732,6 +737,9 @@ sph_status sph_fp8_logits(sph_ctx* ctx, const void* h, sph_tab_type h_type,
  *   out    [rows, d], row stride ld_out; may be x itself, of its type and row
  *          stride.
  *   mean, rstd    fp32 [rows] (out), what sph_layer_norm_grad takes, or NULL.
+ * Fastest, here and in the gradient, where d is a multiple of 8 and each of the
+ * call's rows and parameters starts on eight elements (16 bytes, fp32 32); one that
+ * does not takes the whole call to accesses of one element a thread.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
 sph_status sph_layer_norm(sph_ctx* ctx, const void* x, sph_tab_type x_type,
                           int64_t rows, int64_t d, int64_t ld_x,

@@ -10,13 +10,20 @@
 // tensor core before they are scaled: the MMA warp fills two accumulators in tensor memory in
 // turn, and eight warps add the full one, scaled, to sums in their registers.  A thread has a
 // hidden state and 128 table rows, which share one scale (a kept subset's in runs of 32 do
-// mostly): its factor is one number a block, and a value costs half an instruction.  (With
+// mostly): its factor is one number a block, and a value costs one fused multiply-add.  (With
 // table rows in the lanes, as few hidden states need it, each thread reads a factor a column
 // from shared memory, which gives 128 bytes a cycle and takes twice the MMAs' time: 1024
 // rows x 256000 ids x 4608 1197 us, so 953 to 1026: 2.4 PFLOP/s, where MMAs and copies alone take
 // 678.)  What is left is the additions' latency: eight warps, two a scheduler, read 128 columns
 // of an accumulator and add them (tensor pipe active 44 % of the time, issue slots 42 %); more
 // warps have too few registers for their sums (232 a thread now).
+//
+// Tiles that one factor a block does not serve are computed again by a second kernel, which scales
+// each value by its own table scale: those with a scale outside [2^-50, 2^50] (a block of zeros
+// has 2^-126: with a hidden state of zeros in each 256, 1024 x 256000 x 4608 takes 2091 us), and
+// those with a group of 32 kept ids that meets three blocks of 128 rows or more (1024 x 30412 of
+// 152064 ids x 3584: the first ones 145 us, random ones 3782; with table rows as M, k_fp8_tc.cu
+// without pairs, 171 and 220).
 #include "fp8_tc.cuh"
 #include "rows.cuh"
 

@@ -279,7 +279,9 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_grad_kernel(const NormGr
 }
 
 // Rows too long for the registers: the sums of the columns first (dx may be x or dy), a
-// block for 256 columns and some of the rows, then dx, each row read twice.
+// block for 256 columns and some of the rows, then dx, each row read twice.  Three readings where
+// one is needed, 32 columns an access wherever rows start: 4096 x 16384 bf16 286 us (59 for what
+// has to move), 8000 x 12288 465 (87).
 template <class TX, class TY>
 __global__ void __launch_bounds__(256) norm_columns_kernel(const NormGrad a) {
   __shared__ float part[8][32][17];
@@ -392,10 +394,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(const NormGr
 }
 
 // How a call's rows are divided.  packed: x and dy have 16 bits; ring: they come through shared
-// memory.  Blocks of 256 threads: two an SM, whose threads hold n and g (three that make both
-// twice: 32768 x 4096 bf16 196 us where two took 174, threads of four pieces 220); rows at any
-// address three (325 us, two 383).  Rows of 512 to 1024 columns by blocks too (60000 x 1000 75 us,
-// by warps of four pieces 92).
+// memory.  Blocks of 256 threads: two an SM, whose threads hold n and g (of the form that read the
+// weight for each row, three that make both twice took 196 us where two took 174, threads of four
+// pieces 220); rows at any address three (32768 x 4095 bf16 284 us, two 371).  Rows of 512 to 1024
+// columns by blocks too (60000 x 1000 75 us, by warps of four pieces 92).
 struct GradPlan {
   bool warps, is_long;
   int u, threads, parts;
